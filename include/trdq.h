@@ -25,7 +25,7 @@
  *   - All device work is enqueued asynchronously on `stream`; no entry point
  *     synchronises unless its comment says so.  The online calls (trdq_rotate_quantize and
  *     its _asym, _dense and norm-fused forms, trdq_linear and its _cfg, _act, _asym and split-K
- *     forms, trdq_run_layers, trdq_gemm_i32) allocate no memory; trdq_prepare_weights with a
+ *     forms, trdq_run_layers, trdq_gemm_i32, the trdq_fp8_* and trdq_gated_norm* calls) allocate no memory; trdq_prepare_weights with a
  *     dense-block rotation is the one call that waits for its own work (it frees a scratch buffer).
  *   - The caller owns every tensor it passes.  The library owns only the opaque
  *     trdq_rotation / trdq_weights objects until their _destroy call.  An object belongs to the
@@ -294,6 +294,90 @@ trdq_status trdq_rotate_dense_quantize(const trdq_rotation* rot, int32_t t, cons
  * (fp32) and *n_used (may be NULL).  TRDQ_ERR_GROUP for non-finite inputs or a degenerate draw. */
 trdq_status trdq_greedy_rotation_block(const float* x_calib, int32_t rows, int32_t steps, const double* gauss, float* R_out,
                                        int32_t* n_used);
+
+/* ---- 8-bit floats with a scale for each block of 128 ------------------------------------------------------------
+ * The block quantizer: with a = max |v| over a block,
+ *   scale = fl(a * fl(1/448)),   code = e4m3( fl(v * fl(448 * fl(1/a))) )   (nearest, ties to even; a < 2^-100 counts as 2^-100, a = 0: scale 0)
+ * so that v is close to scale * code.  A block is 128 consecutive channels of one row for activations and 128 x 128 for weights.  The
+ * rotation's block (Eq. 8) is the scale's block, so v may be the rotated row of Eq. 10, G_t(X) or H_t(W), without a pass of its own:
+ * with both sides rotated by the same object and time-step the product is that of trdq_linear.  These calls take the codes and scales
+ * as plain device arrays; 128 x 128-scaled e4m3 weights that come from elsewhere are used as they are.
+ * A NaN or an infinity in X spoils its own row of the product, which becomes NaN, and no other row.
+ *
+ * trdq_fp8_quantize: X_bf16 dev [M, ldx] (ldx >= K, ldx % 8 == 0, 16-byte aligned); codes: dev e4m3 [M, K], 16-byte aligned; scales: dev fp32
+ * [K/128][M], that is scales[b * M + m] (the scales of one channel block side by side, as the product reads them).  rot: NULL for no rotation (t
+ * is then ignored), or an object with rot's K == K (TRDQ_ERR_MISMATCH otherwise, and for the full transform or dense blocks); its act vector of
+ * the group of t is applied as in trdq_rotate_quantize, the fp32 butterflies in the same order.  K % 128 == 0, K <= TRDQ_MAX_K.  M == 0 is a no-op.
+ * trdq_fp8_quantize_weights: the same for W_bf16, dev [N, K] contiguous, N % 16 == 0, with the weight vector of rot's group; codes: dev e4m3
+ * [N, K]; scales: dev fp32 [ceil(N/128)][K/128].  The last row block may be short. */
+trdq_status trdq_fp8_quantize(const trdq_rotation* rot, int32_t t, const void* X_bf16, int64_t ldx, int32_t M, int32_t K, uint8_t* codes,
+                              float* scales, void* stream);
+trdq_status trdq_fp8_quantize_weights(const trdq_rotation* rot, int32_t t, const void* W_bf16, int32_t N, int32_t K, uint8_t* codes,
+                                      float* scales, void* stream);
+
+/* Product of such codes:
+ *   y[m, n] = bf16( act( sum_b sx[b][m] * sw[n / 128][b] * (sum_{k in block b} q[m,k] * qw[n,k]) + bias[n] ) )
+ * The inner sums are fp32 accumulations of the tensor cores, the sum over the blocks is fp32.  Shapes as above; bias_bf16: dev [N], 8-byte
+ * aligned, or NULL; Y_bf16: dev [M, ldy], ldy >= N, ldy % 8 == 0, 16-byte aligned; act as in trdq_linear_act.  Any M from 1 on, N % 16 == 0.  The
+ * order of the sums is fixed for a shape and a device, so equal inputs give equal outputs.  Codes and scales, the weights' too, may come from the
+ * call before on the stream. */
+trdq_status trdq_fp8_linear(const uint8_t* codes, const float* scales, int32_t M, int32_t K, const uint8_t* w_codes, const float* w_scales,
+                            int32_t N, const void* bias_bf16, void* Y_bf16, int64_t ldy, int32_t act, void* stream);
+
+/* ---- norms before and after a block, with its gate and residual scale --------------------------------------------
+ * What lies between the linears of two neighbouring sub-blocks of a transformer, in one pass over memory:
+ *   u = post_norm(branch) o post_weight                  output of the sub-block before, optionally normalised
+ *   r = stream( res_scale * x + gate_s o u )             residual sum, rounded to the stream's type
+ *   h = norm(r) o weight o (1 + scale_s) + shift_s       input of the next sub-block
+ * norm(v) = (v - mean) / sqrt(var + eps) (TRDQ_NORM_LAYER, biased variance) or v / sqrt(mean(v^2) + eps) (TRDQ_NORM_RMS), over the D channels of
+ * a row; s = row / rows_per_sample.  h is the norm of the r that is stored, so trdq_gated_norm_backward, which reads it, differentiates the
+ * function that was computed.  Everything is fp32 inside and rounded once at the outputs (r before its statistics).
+ *   D % 8 == 0, D <= 8192; row strides in elements.  X, R: dev, bf16 (stream_f32 == 0) or fp32; everything else bf16.  Pointers are 16-byte
+ *   aligned and row strides a multiple of 16 bytes.  gate, shift, scale: dev [ceil(M / rows_per_sample)][ld], ld >= D: the three may be column ranges
+ *   of one buffer; weight, post_weight: dev [D].  Any of branch, gate, shift, scale, weight, post_weight may be NULL (no branch: r = res_scale * x, and
+ *   then no gate, post_weight or post_norm: TRDQ_ERR_NULL).  R may be NULL (not stored) or X itself; no other output may overlap an input.
+ *   With shift and one sample (rows_per_sample = M), shift is the bias of an ordinary LayerNorm.
+ * TRDQ_ERR_SHAPE for an unknown norm, a negative or non-finite eps, a non-finite res_scale, rows_per_sample < 1.  M == 0 is a no-op. */
+#define TRDQ_NORM_NONE 0  /* post_norm only */
+#define TRDQ_NORM_LAYER 1
+#define TRDQ_NORM_RMS 2
+typedef struct trdq_gated_norm_op {
+  int32_t M, D, rows_per_sample;
+  int32_t norm, post_norm;
+  int32_t stream_f32;       /* X and R are fp32 in place of bf16 */
+  float eps, res_scale;
+  const void* X;            /* trdq_gated_norm_backward: the stored R */
+  int64_t ldx;
+  const void* branch_bf16;
+  int64_t ldb;
+  const void* gate_bf16;
+  int64_t ld_gate;
+  const void* shift_bf16;
+  int64_t ld_shift;
+  const void* scale_bf16;
+  int64_t ld_scale;
+  const void* weight_bf16;
+  const void* post_weight_bf16;
+} trdq_gated_norm_op;
+
+/* h in bf16: H_bf16 dev [M, ldh]. */
+trdq_status trdq_gated_norm(const trdq_gated_norm_op* op, void* R, int64_t ldr, void* H_bf16, int64_t ldh, void* stream);
+
+/* h, never stored, as the input of the block quantizer above (rotated by rot's group of t, or with rot == NULL as it is): codes e4m3 [M, D] and
+ * scales [D/128][M] as trdq_fp8_quantize writes them, from the fp32 h in place of a bf16 one.  D % 128 == 0. */
+trdq_status trdq_gated_norm_fp8(const trdq_gated_norm_op* op, const trdq_rotation* rot, int32_t t, void* R, int64_t ldr, uint8_t* codes,
+                                float* scales, void* stream);
+
+/* Gradients.  op->X is the stored R; dH_bf16: dev [M, lddh], the gradient of h; dR: dev [M, lddr] in the stream's type, what arrives at r from
+ * elsewhere (the residual path), or NULL.  Outputs, each NULL if not wanted: dX in the stream's type (it may be dR itself), dB_bf16; the
+ * parameters' gradients, fp32: dgate, dshift, dscale [ceil(M / rows_per_sample)][D], dweight, dpost_weight [D] (a gradient of what op
+ * does not have: TRDQ_ERR_NULL).  They are sums over rows in a fixed order, held in `workspace` (dev, 16-byte aligned, at least the bytes that
+ * trdq_gated_norm_backward_workspace reports, TRDQ_ERR_NOMEM if smaller; not needed without them) between two kernels: scratch, its contents do not
+ * matter before or after; calls that may overlap on the GPU need workspaces of their own. */
+trdq_status trdq_gated_norm_backward_workspace(const trdq_gated_norm_op* op, uint64_t* bytes);
+trdq_status trdq_gated_norm_backward(const trdq_gated_norm_op* op, const void* dH_bf16, int64_t lddh, const void* dR, int64_t lddr, void* dX,
+                                     int64_t lddx, void* dB_bf16, int64_t lddb, float* dgate, float* dshift, float* dscale, float* dweight,
+                                     float* dpost_weight, void* workspace, uint64_t workspace_bytes, void* stream);
 
 /* One quantized linear layer of a denoising step: rotate + quantize X into the caller's code and
  * scale buffers, then the integer GEMM with its epilogue into Y (shapes as in the two calls above). */

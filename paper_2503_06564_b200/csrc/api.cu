@@ -162,7 +162,7 @@ static bool aligned_to(const void* p, uintptr_t bytes) { return (reinterpret_cas
 
 // Objects hold device memory and tensor maps of the device they were created on; a call made with another device
 // current would launch there with pointers of the first one.
-static bool on_current_device(int device) {
+bool on_current_device(int device) {
   int cur = -1;
   return cudaGetDevice(&cur) == cudaSuccess && cur == device;
 }
@@ -180,7 +180,7 @@ static trdq_status check_linear_segment(const trdq_weights* w, const void* codes
 
 static trdq_status check_bias(const void* bias_bf16) { return bias_bf16 && !aligned_to(bias_bf16, 2) ? TRDQ_ERR_ALIGN : TRDQ_OK; }
 
-static int find_group(const std::vector<int32_t>& bounds, int32_t t) {
+int find_group(const std::vector<int32_t>& bounds, int32_t t) {
   const int G = static_cast<int>(bounds.size()) - 1;
   for (int g = 0; g < G; ++g)
     if (bounds[g] <= t && t < bounds[g + 1]) return g;

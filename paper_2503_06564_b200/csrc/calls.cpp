@@ -12,6 +12,7 @@
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -34,6 +35,16 @@ struct Entry {
   decltype(&trdq_linear_splitk_workspace) splitk_workspace;
   decltype(&trdq_linear_splitk) linear_splitk;
 } entry;
+
+struct BlockEntry {
+  decltype(&trdq_fp8_quantize) fp8_quantize;
+  decltype(&trdq_fp8_quantize_weights) fp8_quantize_weights;
+  decltype(&trdq_fp8_linear) fp8_linear;
+  decltype(&trdq_gated_norm) gated_norm;
+  decltype(&trdq_gated_norm_fp8) gated_norm_fp8;
+  decltype(&trdq_gated_norm_backward_workspace) gated_norm_backward_workspace;
+  decltype(&trdq_gated_norm_backward) gated_norm_backward;
+} block_entry;
 
 bool no_modes() { return !at::impl::torch_function_mode_enabled() && !c10::impl::TorchDispatchModeTLS::any_modes_set(); }
 
@@ -335,6 +346,253 @@ PyObject* linear_cfg(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- the block-scaled path and the fused norms.  Their tensors have to be on the current device and of the documented shapes and types; anything
+// else goes the general way, which says what is wrong with it.
+
+bool on_device(const at::Tensor& t, c10::DeviceIndex device) { return t.device().index() == device; }
+bool fp8_codes(const at::Tensor& t) { return t.scalar_type() == at::kFloat8_e4m3fn || t.scalar_type() == at::kByte; }
+bool matrix(const at::Tensor& t, int64_t rows, int64_t cols) { return t.dim() == 2 && t.size(0) == rows && t.size(1) == cols && (t.stride(1) == 1 || cols == 1); }
+bool whole(const at::Tensor& t, int64_t rows, int64_t cols) { return matrix(t, rows, cols) && t.is_contiguous(); }
+int64_t leading(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : t.size(1); }
+const at::Tensor& tensor(PyObject* o) { return THPVariable_Unpack(o); }
+bool int32_size(int64_t n) { return n <= std::numeric_limits<int32_t>::max(); }
+// None for no rotation, or its handle
+bool handle_or_none(PyObject* o, void** out) {
+  *out = nullptr;
+  return o == Py_None || handle(o, out);
+}
+
+// (rot or None, t, X, codes, scales, weights)
+PyObject* fp8_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  void* rot;
+  int32_t t, weights;
+  GENERAL_WAY_UNLESS(n == 6 && handle_or_none(a[0], &rot) && number(a[1], &t) && plain(a[2]) && plain_or_none(a[3]) && plain_or_none(a[4]) &&
+                     number(a[5], &weights) && no_modes());
+  const at::Tensor& x = tensor(a[2]);
+  const c10::DeviceIndex device = c10::cuda::current_device();
+  GENERAL_WAY_UNLESS(x.dim() == 2 && x.scalar_type() == at::kBFloat16 && on_device(x, device) && int32_size(x.size(0)) && int32_size(x.size(1)));
+  const int64_t M = x.size(0), K = x.size(1);
+  const int64_t srows = weights ? (M + 127) / 128 : K / 128, scols = weights ? K / 128 : M;
+  GENERAL_WAY_UNLESS(int32_size(srows) && (weights ? x.is_contiguous() : matrix(x, M, K)));
+  GENERAL_WAY_UNLESS(a[3] == Py_None || (on_device(tensor(a[3]), device) && fp8_codes(tensor(a[3])) && whole(tensor(a[3]), M, K)));
+  GENERAL_WAY_UNLESS(a[4] == Py_None || (on_device(tensor(a[4]), device) && tensor(a[4]).scalar_type() == at::kFloat && whole(tensor(a[4]), srows, scols)));
+  Outputs out(a[2]);
+  out.add(a[3], static_cast<int32_t>(M), K, at::kFloat8_e4m3fn);
+  out.add(a[4], static_cast<int32_t>(srows), scols, at::kFloat);
+  const int64_t ldx = leading(x);
+  void* const px = x.data_ptr();
+  void* const s = stream();
+  return out.run([&](void** o) {
+    return weights ? block_entry.fp8_quantize_weights(static_cast<trdq_rotation*>(rot), t, px, static_cast<int32_t>(M), static_cast<int32_t>(K),
+                                                      static_cast<uint8_t*>(o[0]), static_cast<float*>(o[1]), s)
+                   : block_entry.fp8_quantize(static_cast<trdq_rotation*>(rot), t, px, ldx, static_cast<int32_t>(M), static_cast<int32_t>(K),
+                                              static_cast<uint8_t*>(o[0]), static_cast<float*>(o[1]), s);
+  });
+  END_HANDLE_TH_ERRORS
+}
+
+// (codes, scales, w_codes, w_scales, bias, out, act)
+PyObject* fp8_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  int32_t act;
+  GENERAL_WAY_UNLESS(n == 7 && plain(a[0]) && plain(a[1]) && plain(a[2]) && plain(a[3]) && plain_or_none(a[4]) && plain_or_none(a[5]) &&
+                     number(a[6], &act) && no_modes());
+  const at::Tensor &q = tensor(a[0]), &sx = tensor(a[1]), &qw = tensor(a[2]), &sw = tensor(a[3]);
+  const c10::DeviceIndex device = c10::cuda::current_device();
+  GENERAL_WAY_UNLESS(q.dim() == 2 && qw.dim() == 2 && int32_size(q.size(0)) && int32_size(q.size(1)) && int32_size(qw.size(0)));
+  const int64_t M = q.size(0), K = q.size(1), N = qw.size(0);
+  GENERAL_WAY_UNLESS(fp8_codes(q) && whole(q, M, K) && fp8_codes(qw) && whole(qw, N, K) && sx.scalar_type() == at::kFloat && whole(sx, K / 128, M) &&
+                     sw.scalar_type() == at::kFloat && whole(sw, (N + 127) / 128, K / 128));
+  GENERAL_WAY_UNLESS(on_device(q, device) && on_device(sx, device) && on_device(qw, device) && on_device(sw, device));
+  if (a[4] != Py_None) {
+    const at::Tensor& b = tensor(a[4]);
+    GENERAL_WAY_UNLESS(on_device(b, device) && b.scalar_type() == at::kBFloat16 && b.dim() == 1 && b.size(0) == N && b.is_contiguous());
+  }
+  int64_t ldy = N;
+  if (a[5] != Py_None) {
+    const at::Tensor& y = tensor(a[5]);
+    GENERAL_WAY_UNLESS(on_device(y, device) && y.scalar_type() == at::kBFloat16 && matrix(y, M, N));
+    ldy = leading(y);
+  }
+  Outputs out(a[0]);
+  out.add(a[5], static_cast<int32_t>(M), N, at::kBFloat16);
+  void *const pq = q.data_ptr(), *const psx = sx.data_ptr(), *const pqw = qw.data_ptr(), *const psw = sw.data_ptr(), *const bias = pointer(a[4]);
+  void* const s = stream();
+  return out.run([&](void** o) {
+    return block_entry.fp8_linear(static_cast<uint8_t*>(pq), static_cast<float*>(psx), static_cast<int32_t>(M), static_cast<int32_t>(K),
+                                  static_cast<uint8_t*>(pqw), static_cast<float*>(psw), static_cast<int32_t>(N), bias, o[0], ldy, act, s);
+  });
+  END_HANDLE_TH_ERRORS
+}
+
+bool real(PyObject* o, float* out) {
+  if (!PyFloat_CheckExact(o)) return false;
+  *out = static_cast<float>(PyFloat_AS_DOUBLE(o));
+  return true;
+}
+
+// The arguments that the three norm calls share: X, branch, gate, shift, scale, weight, post_weight, norm, post_norm, rows_per_sample, eps, res_scale
+constexpr int kNormArgs = 12;
+bool norm_op(PyObject* const* a, c10::DeviceIndex device, trdq_gated_norm_op* op, int64_t* samples) {
+  if (!plain(a[0])) return false;
+  for (int i = 1; i < 7; ++i)
+    if (!plain_or_none(a[i])) return false;
+  const at::Tensor& x = tensor(a[0]);
+  if (x.dim() != 2 || (x.scalar_type() != at::kBFloat16 && x.scalar_type() != at::kFloat) || !int32_size(x.size(0)) || !int32_size(x.size(1))) return false;
+  const int64_t M = x.size(0), D = x.size(1);
+  if (!matrix(x, M, D) || !on_device(x, device)) return false;
+  int32_t rows = M > 1 ? static_cast<int32_t>(M) : 1;
+  if (a[9] != Py_None && !number(a[9], &rows)) return false;
+  if (rows < 1 || !number(a[7], &op->norm) || !number(a[8], &op->post_norm) || !real(a[10], &op->eps) || !real(a[11], &op->res_scale)) return false;
+  *samples = (M + rows - 1) / rows;
+  op->M = static_cast<int32_t>(M);
+  op->D = static_cast<int32_t>(D);
+  op->rows_per_sample = rows;
+  op->stream_f32 = x.scalar_type() == at::kFloat;
+  op->X = x.data_ptr();
+  op->ldx = leading(x);
+  const void* p[6];
+  int64_t ld[6];
+  for (int i = 1; i < 7; ++i) {
+    p[i - 1] = nullptr;
+    ld[i - 1] = 0;
+    if (a[i] == Py_None) continue;
+    const at::Tensor& t = tensor(a[i]);
+    if (t.scalar_type() != at::kBFloat16 || !on_device(t, device)) return false;
+    if (i < 5 ? !matrix(t, i == 1 ? M : *samples, D) : t.dim() != 1 || t.size(0) != D || (t.stride(0) != 1 && D > 1)) return false;
+    p[i - 1] = t.data_ptr();
+    ld[i - 1] = i < 5 ? leading(t) : 0;
+  }
+  op->branch_bf16 = p[0], op->ldb = ld[0];
+  op->gate_bf16 = p[1], op->ld_gate = ld[1];
+  op->shift_bf16 = p[2], op->ld_shift = ld[2];
+  op->scale_bf16 = p[3], op->ld_scale = ld[3];
+  op->weight_bf16 = p[4];
+  op->post_weight_bf16 = p[5];
+  return true;
+}
+// an output [M, D] of a norm call that may be given, with its row stride
+bool norm_output(PyObject* o, const trdq_gated_norm_op& op, at::ScalarType type, c10::DeviceIndex device, int64_t* ld) {
+  *ld = op.D;
+  if (o == Py_None) return true;
+  if (!plain(o) || !on_device(tensor(o), device) || tensor(o).scalar_type() != type || !matrix(tensor(o), op.M, op.D)) return false;
+  *ld = leading(tensor(o));
+  return true;
+}
+
+// (the shared twelve, resid, out)
+PyObject* gated_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  trdq_gated_norm_op op;
+  int64_t samples, ldr, ldh;
+  const c10::DeviceIndex device = c10::cuda::current_device();
+  GENERAL_WAY_UNLESS(n == kNormArgs + 2 && norm_op(a, device, &op, &samples) && no_modes());
+  const at::ScalarType type = op.stream_f32 ? at::kFloat : at::kBFloat16;
+  GENERAL_WAY_UNLESS(norm_output(a[12], op, type, device, &ldr) && norm_output(a[13], op, at::kBFloat16, device, &ldh));
+  Outputs out(a[0]);
+  out.add(a[12], op.M, op.D, type);
+  out.add(a[13], op.M, op.D, at::kBFloat16);
+  void* const s = stream();
+  return out.run([&](void** o) { return block_entry.gated_norm(&op, o[0], ldr, o[1], ldh, s); });
+  END_HANDLE_TH_ERRORS
+}
+
+// (the shared twelve, rot or None, t, resid, codes, scales)
+PyObject* gated_norm_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  trdq_gated_norm_op op;
+  int64_t samples, ldr, ldc;
+  void* rot;
+  int32_t t;
+  const c10::DeviceIndex device = c10::cuda::current_device();
+  GENERAL_WAY_UNLESS(n == kNormArgs + 5 && norm_op(a, device, &op, &samples) && handle_or_none(a[12], &rot) && number(a[13], &t) && no_modes());
+  const at::ScalarType type = op.stream_f32 ? at::kFloat : at::kBFloat16;
+  GENERAL_WAY_UNLESS(norm_output(a[14], op, type, device, &ldr) && norm_output(a[15], op, at::kFloat8_e4m3fn, device, &ldc) && ldc == op.D);
+  GENERAL_WAY_UNLESS(a[16] == Py_None || (plain(a[16]) && on_device(tensor(a[16]), device) && tensor(a[16]).scalar_type() == at::kFloat &&
+                                          whole(tensor(a[16]), op.D / 128, op.M)));
+  Outputs out(a[0]);
+  out.add(a[14], op.M, op.D, type);
+  out.add(a[15], op.M, op.D, at::kFloat8_e4m3fn);
+  out.add(a[16], op.D / 128, op.M, at::kFloat);
+  void* const s = stream();
+  return out.run([&](void** o) {
+    return block_entry.gated_norm_fp8(&op, static_cast<trdq_rotation*>(rot), t, o[0], ldr, static_cast<uint8_t*>(o[1]), static_cast<float*>(o[2]), s);
+  });
+  END_HANDLE_TH_ERRORS
+}
+
+// (the shared twelve, dH, dR or None): dx, db, dgate, dshift, dscale, dweight, dpost_weight, None where there is no such input
+PyObject* gated_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  trdq_gated_norm_op op;
+  int64_t samples, lddh, lddr;
+  const c10::DeviceIndex device = c10::cuda::current_device();
+  GENERAL_WAY_UNLESS(n == kNormArgs + 2 && norm_op(a, device, &op, &samples) && no_modes());
+  const at::ScalarType type = op.stream_f32 ? at::kFloat : at::kBFloat16;
+  GENERAL_WAY_UNLESS(a[12] != Py_None && norm_output(a[12], op, at::kBFloat16, device, &lddh) && norm_output(a[13], op, type, device, &lddr));
+  uint64_t bytes = 0;
+  bool wanted[7] = {true};  // (a tensor without elements has a null address: what is given decides)
+  for (int i = 1; i < 7; ++i) wanted[i] = a[i] != Py_None;
+  GENERAL_WAY_UNLESS(block_entry.gated_norm_backward_workspace(&op, &bytes) == TRDQ_OK);
+  void *const dh = pointer(a[12]), *const dr = pointer(a[13]);
+  const at::TensorOptions options = tensor(a[0]).options();
+  void* const s = stream();
+  at::Tensor made[7];
+  trdq_status st;
+  {
+    WithoutGil released;
+    at::Tensor workspace;
+    const bool sums = wanted[2] || wanted[3] || wanted[4] || wanted[5] || wanted[6];
+    if (sums) workspace = at::empty({static_cast<int64_t>(bytes > 16 ? bytes : 16)}, options.dtype(at::kByte));
+    for (int i = 0; i < 7; ++i) {
+      if (!wanted[i]) continue;
+      const int64_t rows = i < 2 ? op.M : samples;
+      const at::TensorOptions o = options.dtype(i == 0 ? type : i == 1 ? at::kBFloat16 : at::kFloat);
+      made[i] = i < 5 ? at::empty({rows, op.D}, o) : at::empty({op.D}, o);
+    }
+    auto at_ = [&](int i) { return wanted[i] ? static_cast<float*>(made[i].data_ptr()) : nullptr; };
+    st = block_entry.gated_norm_backward(&op, dh, lddh, dr, dr ? lddr : 0, at_(0), op.D, at_(1), op.D, at_(2), at_(3), at_(4), at_(5), at_(6),
+                                         sums ? workspace.data_ptr() : nullptr, sums ? static_cast<uint64_t>(workspace.numel()) : 0, s);
+  }
+  if (st != TRDQ_OK) return PyLong_FromLong(st);
+  PyObject* const r = PyTuple_New(7);
+  if (!r) return nullptr;
+  for (int i = 0; i < 7; ++i) {
+    PyObject* o = Py_None;
+    if (wanted[i]) {
+      o = THPVariable_Wrap(std::move(made[i]));
+      if (!o) {
+        Py_DECREF(r);
+        return nullptr;
+      }
+    } else {
+      Py_INCREF(o);
+    }
+    PyTuple_SET_ITEM(r, i, o);
+  }
+  return r;
+  END_HANDLE_TH_ERRORS
+}
+
+// (addresses of the library's functions, in the order of BlockEntry)
+PyObject* bind_block(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  void* address[7];
+  if (n != 7) {
+    PyErr_SetString(PyExc_TypeError, "seven addresses");
+    return nullptr;
+  }
+  for (int i = 0; i < 7; ++i) {
+    address[i] = PyLong_AsVoidPtr(a[i]);
+    if (PyErr_Occurred()) return nullptr;
+  }
+  block_entry = {reinterpret_cast<decltype(block_entry.fp8_quantize)>(address[0]),   reinterpret_cast<decltype(block_entry.fp8_quantize_weights)>(address[1]),
+                 reinterpret_cast<decltype(block_entry.fp8_linear)>(address[2]),     reinterpret_cast<decltype(block_entry.gated_norm)>(address[3]),
+                 reinterpret_cast<decltype(block_entry.gated_norm_fp8)>(address[4]), reinterpret_cast<decltype(block_entry.gated_norm_backward_workspace)>(address[5]),
+                 reinterpret_cast<decltype(block_entry.gated_norm_backward)>(address[6])};
+  Py_RETURN_NONE;
+}
+
 // (addresses of the library's functions, in the order of Entry)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   void* address[8];
@@ -355,7 +613,9 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(bind),        METHOD(rotate_quantize), METHOD(norm_rotate_quantize), METHOD(rotate_quantize_asym), METHOD(linear),
-                         METHOD(linear_asym), METHOD(linear_splitk),   METHOD(linear_cfg),           {nullptr, nullptr, 0, nullptr}};
+                         METHOD(linear_asym), METHOD(linear_splitk),   METHOD(linear_cfg),           METHOD(bind_block),
+                         METHOD(fp8_quantize), METHOD(fp8_linear),      METHOD(gated_norm),           METHOD(gated_norm_fp8),       METHOD(gated_norm_backward),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -72,6 +72,9 @@ using PerDeviceFlag = PerDevice<bool>;
 // TRDQ_DEBUG=1: waits for the call's own work and turns a device error or an expired wait into the call's return code.
 trdq_status finish(trdq_status st, void* stream);
 
+bool on_current_device(int device);
+int find_group(const std::vector<int32_t>& bounds, int32_t t);  // -1: t is outside
+
 uint32_t* device_status_word();  // device address of the status word of the current device (nullptr on failure)
 
 // rotate_quantize.cu
@@ -159,6 +162,62 @@ trdq_status launch_gemm_w8_pair(const trdq_weights* w, int g, const GemmSegment 
 // for `sets` time-step groups, the tables of one behind the other
 cudaError_t launch_w4_multipliers(const float* scales, int32_t N, int32_t groups, int32_t n_pad, int sets, int32_t* mult_t, float* base,
                                   cudaStream_t stream);
+
+// fp8_quantize.cu: block-scaled e4m3 codes (fp8.cuh); vec: fused vector of a rotation group, or nullptr for no rotation
+trdq_status launch_fp8_quantize(const void* x_bf16, int64_t ldx, int32_t M, int32_t K, const float* vec, uint8_t* codes, float* scales,
+                                cudaStream_t stream);
+trdq_status launch_fp8_quantize_weights(const void* w_bf16, int32_t N, int32_t K, const float* vec, uint8_t* codes, float* scales,
+                                        cudaStream_t stream);
+
+// gemm_fp8.cu
+struct Fp8Linear {
+  const uint8_t* codes;    // dev e4m3 [M,K]
+  const float* scales;     // dev [K/128][M]
+  const uint8_t* w_codes;  // dev e4m3 [N,K]
+  const float* w_scales;   // dev [ceil(N/128)][K/128]
+  const void* bias_bf16;   // dev [N] or nullptr
+  void* out;               // dev bf16 [M,ld]
+  int64_t ld;
+  int32_t M, N, K, act;
+};
+trdq_status launch_gemm_fp8(const Fp8Linear& p, cudaStream_t stream);
+
+// gated_norm.cu, gated_norm_backward.cu: the fields of trdq_gated_norm_op as the kernels take them
+struct GatedNorm {
+  const void* x;
+  const uint16_t* b;  // nullptr: no branch
+  const uint16_t *gate, *shift, *scale, *weight, *post_weight;
+  int64_t ldx, ldb, ld_gate, ld_shift, ld_scale;
+  void* r;  // nullptr: not stored
+  int64_t ldr;
+  void* out;  // bf16 [M,ldo], or e4m3 [M,D] with `scales`
+  int64_t ldo;
+  float* scales;     // [D/128][M] or nullptr
+  const float* vec;  // with scales: fused vector of the rotation, or nullptr
+  int32_t M, D, rows_per_sample, norm, post;
+  float eps, alpha;
+  bool f32;  // of x and r
+};
+trdq_status launch_gated_norm(const GatedNorm& p, cudaStream_t stream);
+
+struct GatedNormBackward {
+  const void *r, *dr;
+  const uint16_t *b, *dh;
+  const uint16_t *gate, *scale, *weight, *post_weight;
+  int64_t ldr, lddr, ldb, lddh, ld_gate, ld_scale;
+  void* dx;
+  uint16_t* db;
+  int64_t lddx, lddb;
+  float *dgate, *dshift, *dscale, *dweight, *dpost_weight;  // nullptr: not wanted
+  float* workspace;                                         // [3][samples * runs][D]
+  int32_t M, D, rows_per_sample, norm, post;
+  int32_t samples, runs, rows_per_run;  // gated_norm_backward_runs
+  int32_t sample_blocks;                // set by the launcher
+  float eps, alpha;
+  bool f32;
+};
+void gated_norm_backward_runs(int32_t M, int32_t rows_per_sample, int32_t* samples, int32_t* runs, int32_t* rows_per_run);
+trdq_status launch_gated_norm_backward(const GatedNormBackward& p, cudaStream_t stream);
 
 // tensor maps (driver entry point fetched through the runtime; no link-time libcuda dependency)
 // 2-D uint8 row-major [rows, row_bytes-wide], box = 128 bytes x box_rows, 128-byte swizzle.

@@ -33,7 +33,8 @@ EXPORTS = (
     "trdq_rotation_create_full", "trdq_zigzag_permutation", "trdq_rotate_quantize_asym", "trdq_linear_asym",
     "trdq_selftest_wait_expiry", "trdq_rotation_create_dense", "trdq_rotate_dense_workspace", "trdq_rotate_dense_quantize",
     "trdq_greedy_rotation_block", "trdq_linear_act", "trdq_norm_rotate_quantize", "trdq_kernel_choice",
-    "trdq_measure_mma_ceiling",
+    "trdq_measure_mma_ceiling", "trdq_fp8_quantize", "trdq_fp8_quantize_weights", "trdq_fp8_linear", "trdq_gated_norm", "trdq_gated_norm_fp8",
+    "trdq_gated_norm_backward_workspace", "trdq_gated_norm_backward",
 )
 
 
@@ -52,6 +53,14 @@ class LayerOp(C.Structure):
     _fields_ = [("rot", C.c_void_p), ("w", C.c_void_p), ("X_bf16", C.c_void_p), ("ldx", C.c_int64), ("M", C.c_int32),
                 ("codes", C.c_void_p), ("scales", C.c_void_p), ("bias_bf16", C.c_void_p), ("Y_bf16", C.c_void_p),
                 ("ldy", C.c_int64), ("act", C.c_int32), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
+class GatedNormOp(C.Structure):
+    _fields_ = [("M", C.c_int32), ("D", C.c_int32), ("rows_per_sample", C.c_int32), ("norm", C.c_int32), ("post_norm", C.c_int32),
+                ("stream_f32", C.c_int32), ("eps", C.c_float), ("res_scale", C.c_float), ("X", C.c_void_p), ("ldx", C.c_int64),
+                ("branch_bf16", C.c_void_p), ("ldb", C.c_int64), ("gate_bf16", C.c_void_p), ("ld_gate", C.c_int64),
+                ("shift_bf16", C.c_void_p), ("ld_shift", C.c_int64), ("scale_bf16", C.c_void_p), ("ld_scale", C.c_int64),
+                ("weight_bf16", C.c_void_p), ("post_weight_bf16", C.c_void_p)]
 
 
 _lib: Optional[C.CDLL] = None
@@ -101,6 +110,14 @@ def lib() -> C.CDLL:
         l.trdq_greedy_rotation_block.argtypes = [C.POINTER(C.c_float), i32, i32, C.POINTER(C.c_double), C.POINTER(C.c_float),
                                                  C.POINTER(i32)]
         l.trdq_device_status.argtypes = [C.POINTER(C.c_uint32)]
+        op = C.POINTER(GatedNormOp)
+        l.trdq_fp8_quantize.argtypes = [vp, i32, vp, i64, i32, i32, vp, vp, vp]
+        l.trdq_fp8_quantize_weights.argtypes = [vp, i32, vp, i32, i32, vp, vp, vp]
+        l.trdq_fp8_linear.argtypes = [vp, vp, i32, i32, vp, vp, i32, vp, vp, i64, i32, vp]
+        l.trdq_gated_norm.argtypes = [op, vp, i64, vp, i64, vp]
+        l.trdq_gated_norm_fp8.argtypes = [op, vp, i32, vp, i64, vp, vp, vp]
+        l.trdq_gated_norm_backward_workspace.argtypes = [op, C.POINTER(C.c_uint64)]
+        l.trdq_gated_norm_backward.argtypes = [op, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, C.c_uint64, vp]
         _lib = l
     return _lib
 
@@ -155,6 +172,9 @@ def _calls():
             native.bind(*(C.cast(f, C.c_void_p).value for f in (
                 l.trdq_rotate_quantize, l.trdq_norm_rotate_quantize, l.trdq_rotate_quantize_asym, l.trdq_linear_act, l.trdq_linear_cfg,
                 l.trdq_linear_asym, l.trdq_linear_splitk_workspace, l.trdq_linear_splitk)))
+            native.bind_block(*(C.cast(f, C.c_void_p).value for f in (
+                l.trdq_fp8_quantize, l.trdq_fp8_quantize_weights, l.trdq_fp8_linear, l.trdq_gated_norm, l.trdq_gated_norm_fp8,
+                l.trdq_gated_norm_backward_workspace, l.trdq_gated_norm_backward)))
         except ImportError as e:
             warnings.warn(f"the native calls cannot be used, calls take about twice the host time: {e}; build them with "
                           "`python -m paper_2503_06564_b200.build`")
@@ -521,6 +541,235 @@ def trdq_gemm_i32(w: Weights, t: int, codes, out=None):
     ld = int(out.stride(0)) if M > 1 else w.N
     _check(lib().trdq_gemm_i32(w._h, int(t), _ptr(codes), M, _ptr(out), ld, _stream()), "trdq_gemm_i32")
     return out
+
+
+# ---- 8-bit floats with a scale for each block of 128 ----
+def _here(where: str, *tensors) -> None:
+    """These calls keep no object that would know its device: their tensors have to be on the current one."""
+    import torch
+    for x in tensors:
+        if x is not None and (not x.is_cuda or x.device.index != torch.cuda.current_device()):
+            raise TrdqError(10, f"{where} (a tensor is not on the current device)")
+
+
+def _expect(where: str, x, shape, *dtypes) -> None:
+    """x has this shape and one of these types, its last dimension side by side."""
+    if x is None:
+        return
+    assert x.dtype in dtypes, f"{where}: {x.dtype} where {dtypes} is expected"
+    if tuple(x.shape) != tuple(shape):
+        raise TrdqError(2, f"{where} (shape {tuple(x.shape)} where {tuple(shape)} is expected)")
+    assert x.numel() == 0 or x.stride(-1) == 1 or x.shape[-1] == 1, f"{where}: elements of a row do not lie side by side"
+
+
+def _whole(where: str, *tensors) -> None:
+    assert all(x is None or x.is_contiguous() for x in tensors), f"{where}: a tensor that has to be contiguous is not"
+
+
+def _ld(x) -> int:
+    return int(x.stride(0)) if x.shape[0] > 1 else int(x.shape[1])
+
+
+def _rotation(rot: Optional[Rotation], where: str) -> Optional[int]:
+    """Handle of a rotation, None for none.  A closed one is an error: its null handle would mean no rotation."""
+    if rot is None:
+        return None
+    if not rot._h:
+        raise TrdqError(1, f"{where} (the rotation is closed)")
+    return rot._h.value
+
+
+def _fp8_types():
+    import torch
+    return torch.float8_e4m3fn, torch.uint8
+
+
+def trdq_fp8_quantize(X_bf16, rot: Optional[Rotation] = None, t: int = 0, codes=None, scales=None):
+    """(codes e4m3 [M,K], scales fp32 [K/128,M]) of the rows of X, rotated by `rot` at time-step t if it is given."""
+    where = "trdq_fp8_quantize"
+    done = (_native or _calls()).fp8_quantize(_rotation(rot, where), t, X_bf16, codes, scales, 0)
+    if done is not None:
+        return _done(done, where)
+    import torch
+    assert X_bf16.dim() == 2 and X_bf16.dtype == torch.bfloat16
+    M, K = int(X_bf16.shape[0]), int(X_bf16.shape[1])
+    _here(where, X_bf16, codes, scales)
+    _expect(where, X_bf16, (M, K), torch.bfloat16)
+    if codes is None:
+        codes = torch.empty((M, K), dtype=torch.float8_e4m3fn, device=X_bf16.device)
+    if scales is None:
+        scales = torch.empty((K // 128, M), dtype=torch.float32, device=X_bf16.device)
+    _expect(where, codes, (M, K), *_fp8_types())
+    _expect(where, scales, (K // 128, M), torch.float32)
+    _whole(where, codes, scales)
+    _check(lib().trdq_fp8_quantize(_rotation(rot, where), int(t), _ptr(X_bf16), _ld(X_bf16), M, K, _ptr(codes), _ptr(scales), _stream()), where)
+    return codes, scales
+
+
+def trdq_fp8_quantize_weights(W_bf16, rot: Optional[Rotation] = None, t: int = 0, codes=None, scales=None):
+    """(codes e4m3 [N,K], scales fp32 [ceil(N/128),K/128]) of a weight matrix, for the group of time-step t if `rot` is given."""
+    where = "trdq_fp8_quantize_weights"
+    done = (_native or _calls()).fp8_quantize(_rotation(rot, where), t, W_bf16, codes, scales, 1)
+    if done is not None:
+        return _done(done, where)
+    import torch
+    assert W_bf16.dim() == 2 and W_bf16.dtype == torch.bfloat16
+    N, K = int(W_bf16.shape[0]), int(W_bf16.shape[1])
+    _here(where, W_bf16, codes, scales)
+    if codes is None:
+        codes = torch.empty((N, K), dtype=torch.float8_e4m3fn, device=W_bf16.device)
+    if scales is None:
+        scales = torch.empty(((N + 127) // 128, K // 128), dtype=torch.float32, device=W_bf16.device)
+    _expect(where, codes, (N, K), *_fp8_types())
+    _expect(where, scales, ((N + 127) // 128, K // 128), torch.float32)
+    _whole(where, W_bf16, codes, scales)
+    _check(lib().trdq_fp8_quantize_weights(_rotation(rot, where), int(t), _ptr(W_bf16), N, K, _ptr(codes), _ptr(scales), _stream()), where)
+    return codes, scales
+
+
+def trdq_fp8_linear(codes, scales, w_codes, w_scales, bias_bf16=None, out=None, act: int = ACT_NONE):
+    """bf16 [M,N] product of block-scaled codes, with bias and activation."""
+    where = "trdq_fp8_linear"
+    done = (_native or _calls()).fp8_linear(codes, scales, w_codes, w_scales, bias_bf16, out, act)
+    if done is not None:
+        return _done(done, where)
+    import torch
+    assert codes.dim() == 2 and w_codes.dim() == 2
+    M, K, N = int(codes.shape[0]), int(codes.shape[1]), int(w_codes.shape[0])
+    _here(where, codes, scales, w_codes, w_scales, bias_bf16, out)
+    if out is None:
+        out = torch.empty((M, N), dtype=torch.bfloat16, device=codes.device)
+    _expect(where, codes, (M, K), *_fp8_types())
+    _expect(where, scales, (K // 128, M), torch.float32)
+    _expect(where, w_codes, (N, K), *_fp8_types())
+    _expect(where, w_scales, ((N + 127) // 128, K // 128), torch.float32)
+    _expect(where, bias_bf16, (N,), torch.bfloat16)
+    _expect(where, out, (M, N), torch.bfloat16)
+    _whole(where, codes, scales, w_codes, w_scales, bias_bf16)
+    _check(lib().trdq_fp8_linear(_ptr(codes), _ptr(scales), M, K, _ptr(w_codes), _ptr(w_scales), N, _ptr(bias_bf16), _ptr(out), _ld(out), int(act),
+                                 _stream()), where)
+    return out
+
+
+# ---- norms before and after a block, with its gate and residual scale ----
+NORM_NONE, NORM_LAYER, NORM_RMS = 0, 1, 2
+
+
+def _gated_norm_op(where, X, branch, gate, shift, scale, weight, post_weight, norm, post_norm, rows_per_sample, eps, res_scale) -> GatedNormOp:
+    import torch
+    assert X.dim() == 2 and X.dtype in (torch.bfloat16, torch.float32)
+    M, D = int(X.shape[0]), int(X.shape[1])
+    rows = max(M, 1) if rows_per_sample is None else int(rows_per_sample)
+    if rows < 1:
+        raise TrdqError(2, f"{where} (rows_per_sample)")
+    samples = (M + rows - 1) // rows
+    _here(where, X, branch, gate, shift, scale, weight, post_weight)
+    _expect(where, X, (M, D), X.dtype)
+    _expect(where, branch, (M, D), torch.bfloat16)
+    for p in (gate, shift, scale):
+        _expect(where, p, (samples, D), torch.bfloat16)
+    for p in (weight, post_weight):
+        _expect(where, p, (D,), torch.bfloat16)
+
+    def ld(p):
+        return 0 if p is None else _ld(p)
+
+    return GatedNormOp(M, D, rows, int(norm), int(post_norm), int(X.dtype == torch.float32), float(eps), float(res_scale), _ptr(X), _ld(X), _ptr(branch),
+                       ld(branch), _ptr(gate), ld(gate), _ptr(shift), ld(shift), _ptr(scale), ld(scale), _ptr(weight), _ptr(post_weight))
+
+
+def trdq_gated_norm(X, branch_bf16=None, gate=None, shift=None, scale=None, weight=None, post_weight=None, norm: int = NORM_LAYER,
+                    post_norm: int = NORM_NONE, rows_per_sample: Optional[int] = None, eps: float = 1e-6, res_scale: float = 1.0, resid=None, out=None):
+    """(R, H): R = res_scale * X + gate o post_norm(branch) o post_weight in X's type (`resid`: where to, X itself if wanted), and the bf16
+    H = norm(R) o weight o (1 + scale) + shift.  gate, shift, scale: bf16 [samples, D], columns of a wider buffer if wanted."""
+    where = "trdq_gated_norm"
+    done = (_native or _calls()).gated_norm(X, branch_bf16, gate, shift, scale, weight, post_weight, norm, post_norm, rows_per_sample, eps, res_scale,
+                                            resid, out)
+    if done is not None:
+        return _done(done, where)
+    import torch
+    op = _gated_norm_op(where, X, branch_bf16, gate, shift, scale, weight, post_weight, norm, post_norm, rows_per_sample, eps, res_scale)
+    _here(where, resid, out)
+    if resid is None:
+        resid = torch.empty((op.M, op.D), dtype=X.dtype, device=X.device)
+    if out is None:
+        out = torch.empty((op.M, op.D), dtype=torch.bfloat16, device=X.device)
+    _expect(where, resid, (op.M, op.D), X.dtype)
+    _expect(where, out, (op.M, op.D), torch.bfloat16)
+    _check(lib().trdq_gated_norm(C.byref(op), _ptr(resid), _ld(resid), _ptr(out), _ld(out), _stream()), where)
+    return resid, out
+
+
+def trdq_gated_norm_fp8(rot: Optional[Rotation], t: int, X, branch_bf16=None, gate=None, shift=None, scale=None, weight=None, post_weight=None,
+                        norm: int = NORM_LAYER, post_norm: int = NORM_NONE, rows_per_sample: Optional[int] = None, eps: float = 1e-6,
+                        res_scale: float = 1.0, resid=None, codes=None, scales=None):
+    """trdq_gated_norm with H rotated (by `rot`, if it is given) and quantized in place of written: (R, codes e4m3 [M,D], scales fp32 [D/128,M])."""
+    where = "trdq_gated_norm_fp8"
+    done = (_native or _calls()).gated_norm_fp8(X, branch_bf16, gate, shift, scale, weight, post_weight, norm, post_norm, rows_per_sample, eps, res_scale,
+                                                _rotation(rot, where), t, resid, codes, scales)
+    if done is not None:
+        return _done(done, where)
+    import torch
+    op = _gated_norm_op(where, X, branch_bf16, gate, shift, scale, weight, post_weight, norm, post_norm, rows_per_sample, eps, res_scale)
+    _here(where, resid, codes, scales)
+    if resid is None:
+        resid = torch.empty((op.M, op.D), dtype=X.dtype, device=X.device)
+    if codes is None:
+        codes = torch.empty((op.M, op.D), dtype=torch.float8_e4m3fn, device=X.device)
+    if scales is None:
+        scales = torch.empty((op.D // 128, op.M), dtype=torch.float32, device=X.device)
+    _expect(where, resid, (op.M, op.D), X.dtype)
+    _expect(where, codes, (op.M, op.D), *_fp8_types())
+    _expect(where, scales, (op.D // 128, op.M), torch.float32)
+    _whole(where, codes, scales)
+    _check(lib().trdq_gated_norm_fp8(C.byref(op), _rotation(rot, where), int(t), _ptr(resid), _ld(resid), _ptr(codes), _ptr(scales), _stream()),
+           where)
+    return resid, codes, scales
+
+
+def trdq_gated_norm_backward(R, branch_bf16, dH_bf16, dR=None, gate=None, shift=None, scale=None, weight=None, post_weight=None,
+                             norm: int = NORM_LAYER, post_norm: int = NORM_NONE, rows_per_sample: Optional[int] = None, eps: float = 1e-6,
+                             res_scale: float = 1.0, dX=None, dB=None, workspace=None) -> dict:
+    """Gradients of trdq_gated_norm from the stored R, the gradient of H and (or None) what arrives at R from elsewhere: dx in R's type, db in bf16 and
+    those of the parameters that are given in fp32, under the names dx, db, dgate, dshift, dscale, dweight, dpost_weight (None: no such input)."""
+    where = "trdq_gated_norm_backward"
+    names = ("dx", "db", "dgate", "dshift", "dscale", "dweight", "dpost_weight")
+    if dX is None and dB is None and workspace is None:
+        done = (_native or _calls()).gated_norm_backward(R, branch_bf16, gate, shift, scale, weight, post_weight, norm, post_norm, rows_per_sample, eps,
+                                                         res_scale, dH_bf16, dR)
+        if done is not None:
+            return dict(zip(names, _done(done, where)))
+    import torch
+    op = _gated_norm_op(where, R, branch_bf16, gate, shift, scale, weight, post_weight, norm, post_norm, rows_per_sample, eps, res_scale)
+    M, D, dev = op.M, op.D, R.device
+    samples = (M + op.rows_per_sample - 1) // op.rows_per_sample
+    _here(where, dH_bf16, dR, dX, dB, workspace)
+    if dX is None:
+        dX = torch.empty((M, D), dtype=R.dtype, device=dev)
+    if dB is None and branch_bf16 is not None:
+        dB = torch.empty((M, D), dtype=torch.bfloat16, device=dev)
+    _expect(where, dH_bf16, (M, D), torch.bfloat16)
+    _expect(where, dR, (M, D), R.dtype)
+    _expect(where, dX, (M, D), R.dtype)
+    _expect(where, dB, (M, D), torch.bfloat16)
+
+    def grad(p, *shape):
+        return None if p is None else torch.empty(shape, dtype=torch.float32, device=dev)
+
+    dgate, dshift, dscale = grad(gate, samples, D), grad(shift, samples, D), grad(scale, samples, D)
+    dweight, dpost_weight = grad(weight, D), grad(post_weight, D)
+    if workspace is None and any(g is not None for g in (dgate, dshift, dscale, dweight, dpost_weight)):
+        n = C.c_uint64(0)
+        _check(lib().trdq_gated_norm_backward_workspace(C.byref(op), C.byref(n)), where)
+        workspace = torch.empty((max(int(n.value), 16),), dtype=torch.uint8, device=dev)
+
+    def ld(p):
+        return 0 if p is None else _ld(p)
+
+    _check(lib().trdq_gated_norm_backward(C.byref(op), _ptr(dH_bf16), ld(dH_bf16), _ptr(dR), ld(dR), _ptr(dX), ld(dX), _ptr(dB), ld(dB), _ptr(dgate),
+                                          _ptr(dshift), _ptr(dscale), _ptr(dweight), _ptr(dpost_weight), _ptr(workspace),
+                                          0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()), where)
+    return dict(zip(names, (dX, dB, dgate, dshift, dscale, dweight, dpost_weight)))
 
 
 class LayerList:
