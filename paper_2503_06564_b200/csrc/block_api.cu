@@ -159,7 +159,7 @@ trdq_status trdq_gated_norm_backward_workspace(const trdq_gated_norm_op* op, uin
   *bytes = 0;
   if (op->M == 0) return TRDQ_OK;
   int32_t samples, runs, rows;
-  gated_norm_backward_runs(op->M, op->rows_per_sample, &samples, &runs, &rows);
+  gated_norm_backward_runs(op->M, op->D, op->rows_per_sample, &samples, &runs, &rows);
   *bytes = 3ull * static_cast<uint64_t>(samples) * static_cast<uint64_t>(runs) * static_cast<uint64_t>(op->D) * sizeof(float);
   return TRDQ_OK;
 }
@@ -188,7 +188,7 @@ trdq_status trdq_gated_norm_backward(const trdq_gated_norm_op* op, const void* d
   if (st != TRDQ_OK) return st;
   if (dX && dX == dR && lddx != lddr && op->M > 1) return TRDQ_ERR_SHAPE;
   GatedNormBackward p;
-  gated_norm_backward_runs(op->M, op->rows_per_sample, &p.samples, &p.runs, &p.rows_per_run);
+  gated_norm_backward_runs(op->M, op->D, op->rows_per_sample, &p.samples, &p.runs, &p.rows_per_run);
   if (dgate || dshift || dscale || dweight || dpost_weight) {
     uint64_t need = 0;
     trdq_gated_norm_backward_workspace(op, &need);

@@ -21,7 +21,7 @@ struct Fp8Factor {
 // amax: the block's maximum; a NaN among the values leaves no trace in it, but becomes a NaN code by itself.
 __device__ __forceinline__ Fp8Factor fp8_factor(float amax) {
   const float a = fmaxf(amax, kFp8Tiny);
-  return Fp8Factor{amax > 0.0f ? __fmul_rn(a, kFp8InvMax) : 0.0f, __fmul_rn(__fdiv_rn(1.0f, a), kFp8Max)};
+  return Fp8Factor{amax > 0.0f ? __fmul_rn(a, kFp8InvMax) : 0.0f, __fmul_rn(__frcp_rn(a), kFp8Max)};
 }
 
 // Two codes, lo in the low byte; magnitudes beyond 448 (one rounding of v * mul) become 448.

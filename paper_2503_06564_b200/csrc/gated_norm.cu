@@ -5,12 +5,12 @@
 // backward pass first of all, sees the function that was computed.  h goes out in bf16, or, never stored, through the rotation of Eq. 10
 // and the block quantizer of fp8.cuh.
 //
-// A team of W warps holds a row in registers, CH chunks of eight channels a lane, so that each input is read once and the variance is the mean of
-// squared deviations, not a difference of two large sums.  Sixteen lanes hold a 128-block: three butterfly stages in a thread, four
-// by shuffle, in the order h = 1, 2, ..., 64 of the other kernels.
-// What bounds it: memory.  8 bytes a channel with a bf16 stream, 7 with codes.
+// A CTA holds one row in registers, eight channels a thread (sixteen above 4096), so that each input is read once and the variance is
+// a mean of squared deviations, not a difference of two large sums.  It walks down a run of neighbouring rows: the next row's inputs are
+// requested before this one's are used, and the sample's parameters stay in registers until the sample changes.  Sixteen lanes hold a
+// 128-block of the rotation: three butterfly stages in a thread, four by shuffle, in the order h = 1, 2, ..., 64 of the other kernels.
+// What bounds it: memory, 8 bytes a channel with a bf16 stream, 7 with codes, and close behind it instruction issue.
 #include <algorithm>
-#include <type_traits>
 
 #include "fp8.cuh"
 #include "gated_norm.cuh"
@@ -18,8 +18,6 @@
 
 namespace trdq {
 namespace {
-
-constexpr int kWarps = 8;
 
 __device__ __forceinline__ Chunk load_vec(const float* vec, int chunk) {
   const float4 a = __ldg(reinterpret_cast<const float4*>(vec) + 2 * chunk), b = __ldg(reinterpret_cast<const float4*>(vec) + 2 * chunk + 1);
@@ -60,156 +58,167 @@ __device__ __forceinline__ float chunk_absmax(const Chunk& c) {
   return m;
 }
 
-// v -> (v - mean) or v, and 1 / sqrt(mean square + eps) of the result; chunks outside the row stay zero.
-template <int W, int CH>
-__device__ __forceinline__ float centre(Chunk (&v)[CH], const bool (&in)[CH], int kind, float d, float eps, TeamSum<W>& team) {
-  if (kind == TRDQ_NORM_LAYER) {
-    float s = 0.0f;
-#pragma unroll
-    for (int j = 0; j < CH; ++j) s = __fadd_rn(s, chunk_sum(v[j]));
-    const float mean = __fdiv_rn(team.sum(s), d);
-#pragma unroll
-    for (int j = 0; j < CH; ++j)
-      if (in[j]) v[j] = chunk_shift(v[j], -mean);
-  }
-  float q = 0.0f;
-#pragma unroll
-  for (int j = 0; j < CH; ++j) q = __fadd_rn(q, chunk_dot(v[j], v[j]));
-  return __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fdiv_rn(team.sum(q), d), eps)));
-}
-
-template <int W, int CH, bool F32, bool FP8>
-__global__ void __launch_bounds__(32 * kWarps) gated_norm_kernel(const GatedNorm p) {
-  constexpr int kTeams = kWarps / W;
-  __shared__ float slots[kTeams][TeamSum<W>::kFloats];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int team_id = warp / W;
-  TeamSum<W> team(slots[team_id], team_id, warp % W);
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * kTeams + team_id;
+template <int CH, bool F32, bool FP8>
+__global__ void __launch_bounds__(32 * kRowWarps) gated_norm_kernel(const GatedNorm p, int32_t rows_per_cta) {
+  __shared__ float4 slots[RowSum::kSlots];
+  RowSum sums(slots);
+  const int lane = threadIdx.x & 31;
+  const float inv_d = __fdiv_rn(1.0f, static_cast<float>(p.D));
+  const int64_t row0 = static_cast<int64_t>(blockIdx.x) * rows_per_cta;
+  const int rows = static_cast<int>(min(static_cast<int64_t>(rows_per_cta), p.M - row0));
   griddep_launch_dependents();
   griddep_wait();
-  if (row >= p.M) return;  // whole teams
-  const int64_t s = row / p.rows_per_sample;
-  const int chunks = p.D / 8;
-  const int first = (warp % W) * 32 + lane;
-  const float d = static_cast<float>(p.D);
 
+  // Addresses of this thread's chunks, moved on row by row.
+  constexpr int kBytes = F32 ? 4 : 2;
   bool in[CH];
-  StreamChunk<F32> x[CH];
-  uint4 b[CH];
-  const void* const xrow = stream_row(p.x, row, p.ldx, F32);
-  const uint16_t* const brow = p.b ? p.b + row * p.ldb : nullptr;
+  int at[CH];
+  const char *x_at[CH], *b_at[CH];
+  char *r_at[CH], *out_at[CH];
+  float* scale_at[CH];
 #pragma unroll
   for (int j = 0; j < CH; ++j) {
-    const int c = first + j * 32 * W;
-    in[j] = c < chunks;
-    x[j].clear();
-    b[j] = zero4();
-    if (in[j]) {
-      x[j].load(xrow, c);
-      if (brow) b[j] = *(reinterpret_cast<const uint4*>(brow) + c);
-    }
+    at[j] = static_cast<int>(threadIdx.x + j * blockDim.x);
+    in[j] = at[j] < p.D / 8;
+    x_at[j] = stream_at(p.x, row0, p.ldx, at[j], F32);
+    b_at[j] = stream_at(p.b, row0, p.ldb, at[j], false);
+    r_at[j] = stream_at(p.r, row0, p.ldr, at[j], F32);
+    out_at[j] = static_cast<char*>(p.out) + (row0 * p.ldo + 8 * at[j]) * (FP8 ? 1 : 2);
+    if constexpr (FP8) scale_at[j] = p.scales + static_cast<int64_t>(at[j] / 16) * p.M + row0;
   }
-  Chunk v[CH];
-  if (brow) {
+  const Chunk none{{make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)}};
+
+  StreamChunk<F32> next_x[CH];
+  uint4 next_b[CH];
 #pragma unroll
-    for (int j = 0; j < CH; ++j) v[j] = widen(b[j]);
+  for (int j = 0; j < CH; ++j) {  // what is not loaded (lanes outside the row, no branch) stays zero
+    next_x[j].clear();
+    next_b[j] = zero4();
+  }
+  auto fetch = [&](bool valid) {
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+      if (valid && in[j]) {
+        next_x[j].load(x_at[j]);
+        if (p.b) next_b[j] = *reinterpret_cast<const uint4*>(b_at[j]);
+      }
+      x_at[j] += p.ldx * kBytes;
+      b_at[j] += p.ldb * 2;
+    }
+  };
+  fetch(rows > 0);
+
+  Chunk gate[CH], gain[CH], shift[CH];  // gate o pw, (1 + scale) o w, shift of this thread's columns
+  int until = 0;                        // rows from row0 on that these hold for
+  const float2 alpha2 = make_float2(p.alpha, p.alpha);
+  for (int i = 0; i < rows; ++i) {
+    if (i >= until) {
+      const int64_t s = (row0 + i) / p.rows_per_sample;
+      until = static_cast<int>(min((s + 1) * p.rows_per_sample - row0, static_cast<int64_t>(rows)));
+      uint4 g[CH], sc[CH], sh[CH], w[CH], pw[CH];  // all requested before the first is used
+#pragma unroll
+      for (int j = 0; j < CH; ++j) {
+        const int c = in[j] ? at[j] : 0;
+        g[j] = p.gate ? load_param(p.gate + s * p.ld_gate, c) : zero4();
+        sc[j] = p.scale ? load_param(p.scale + s * p.ld_scale, c) : zero4();
+        sh[j] = p.shift ? load_param(p.shift + s * p.ld_shift, c) : zero4();
+        w[j] = p.weight ? load_param(p.weight, c) : zero4();
+        pw[j] = p.post_weight ? load_param(p.post_weight, c) : zero4();
+      }
+#pragma unroll
+      for (int j = 0; j < CH; ++j) {
+        gate[j] = p.gate ? widen(g[j]) : chunk_shift(none, 1.0f);
+        if (p.post_weight) gate[j] = chunk_mul(gate[j], widen(pw[j]));
+        gain[j] = chunk_shift(widen(sc[j]), 1.0f);
+        if (p.weight) gain[j] = chunk_mul(gain[j], widen(w[j]));
+        shift[j] = widen(sh[j]);
+        if (!in[j]) shift[j] = none;
+      }
+    }
+    StreamChunk<F32> x[CH];
+    Chunk v[CH];
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+      x[j] = next_x[j];
+      v[j] = widen(next_b[j]);
+    }
+    fetch(i + 1 < rows);
+
     if (p.post != TRDQ_NORM_NONE) {
-      const float f = centre<W, CH>(v, in, p.post, d, p.eps, team);
+      const float f = row_centre(v, in, p.post, inv_d, p.eps, sums);
 #pragma unroll
       for (int j = 0; j < CH; ++j) v[j] = chunk_scale(v[j], f);
     }
 #pragma unroll
     for (int j = 0; j < CH; ++j) {
-      const int c = first + j * 32 * W;
-      if (!in[j]) continue;
-      if (p.post_weight) v[j] = chunk_mul(v[j], widen(load_param(p.post_weight, c)));
-      if (p.gate) v[j] = chunk_mul(v[j], widen(load_param(p.gate + s * p.ld_gate, c)));
+      const Chunk xv = x[j].value();
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[j].p[k] = __ffma2_rn(v[j].p[k], gate[j].p[k], __fmul2_rn(xv.p[k], alpha2));
+      x[j].set(v[j]);
+      v[j] = x[j].value();
+      if (p.r && in[j]) x[j].store(r_at[j]);
+      r_at[j] += p.ldr * kBytes;
     }
-  } else {
+    const float f = row_centre(v, in, p.norm, inv_d, p.eps, sums);
 #pragma unroll
-    for (int j = 0; j < CH; ++j) v[j] = Chunk{{make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)}};
-  }
-  const float2 alpha2 = make_float2(p.alpha, p.alpha);
+    for (int j = 0; j < CH; ++j) {
+      v[j] = chunk_fma(chunk_scale(v[j], f), gain[j], shift[j]);
+      if constexpr (FP8) {
+        if (p.vec) {
+          if (in[j]) v[j] = chunk_mul(v[j], load_vec(p.vec, at[j]));
+          wht128_lanes16(v[j], lane);
+        }
+        float m = chunk_absmax(v[j]);
 #pragma unroll
-  for (int j = 0; j < CH; ++j) {
-    const Chunk xv = x[j].value();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[j].p[i] = brow ? __fadd2_rn(__fmul2_rn(xv.p[i], alpha2), v[j].p[i]) : __fmul2_rn(xv.p[i], alpha2);
-    x[j].set(v[j]);
-    v[j] = x[j].value();
-  }
-  if (p.r) {
-    void* const rrow = stream_row(p.r, row, p.ldr, F32);
-#pragma unroll
-    for (int j = 0; j < CH; ++j)
-      if (in[j]) x[j].store(rrow, first + j * 32 * W);
-  }
-
-  const float f = centre<W, CH>(v, in, p.norm, d, p.eps, team);
-#pragma unroll
-  for (int j = 0; j < CH; ++j) {
-    const int c = first + j * 32 * W;
-    v[j] = chunk_scale(v[j], f);
-    if (in[j]) {
-      if (p.weight) v[j] = chunk_mul(v[j], widen(load_param(p.weight, c)));
-      if (p.scale) v[j] = chunk_mul(v[j], chunk_shift(widen(load_param(p.scale + s * p.ld_scale, c)), 1.0f));
-      if (p.shift) {
-        const Chunk sh = widen(load_param(p.shift + s * p.ld_shift, c));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[j].p[i] = __fadd2_rn(v[j].p[i], sh.p[i]);
+        for (int k = 1; k < 16; k <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
+        const Fp8Factor q = fp8_factor(m);
+        if (in[j]) {
+          const Chunk o = chunk_scale(v[j], q.mul);
+          *reinterpret_cast<uint2*>(out_at[j]) = make_uint2(fp8_pack4(o.p[0], o.p[1]), fp8_pack4(o.p[2], o.p[3]));
+          if ((lane & 15) == 0) *scale_at[j] = q.scale;
+        }
+        ++scale_at[j];
+      } else {
+        if (in[j]) *reinterpret_cast<uint4*>(out_at[j]) = narrow(v[j]);
       }
-    }
-    if constexpr (FP8) {
-      if (p.vec) {
-        if (in[j]) v[j] = chunk_mul(v[j], load_vec(p.vec, c));
-        wht128_lanes16(v[j], lane);
-      }
-      float m = chunk_absmax(v[j]);
-#pragma unroll
-      for (int k = 1; k < 16; k <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
-      const Fp8Factor q = fp8_factor(m);
-      if (in[j]) {
-        const Chunk o = chunk_scale(v[j], q.mul);
-        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.out) + row * p.D + 8 * c) = make_uint2(fp8_pack4(o.p[0], o.p[1]), fp8_pack4(o.p[2], o.p[3]));
-        if ((lane & 15) == 0) p.scales[static_cast<int64_t>(c / 16) * p.M + row] = q.scale;
-      }
-    } else {
-      if (in[j]) *(reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + row * p.ldo) + c) = narrow(v[j]);
+      out_at[j] += p.ldo * (FP8 ? 1 : 2);
     }
   }
 }
 
-template <int W, int CH>
-cudaError_t launch_shape(const GatedNorm& p, cudaStream_t stream) {
-  constexpr int kTeams = kWarps / W;
-  const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(p.M) + kTeams - 1) / kTeams);
+template <int CH, bool F32, bool FP8>
+cudaError_t launch(const GatedNorm& p, int dev, int sms, cudaStream_t stream) {
+  // CTAs of this width that an SM holds at once
+  static PerDevice<int> resident[kRowWarps];
+  const int threads = row_threads(p.D);
+  int per_sm = resident[threads / 32 - 1].get(dev);
+  if (per_sm == 0) {
+    const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, gated_norm_kernel<CH, F32, FP8>, threads, 0);
+    if (e != cudaSuccess) return e;
+    per_sm = std::max(1, per_sm);
+    resident[threads / 32 - 1].set(dev, per_sm);
+  }
+  const int64_t ctas = std::min<int64_t>(p.M, static_cast<int64_t>(per_sm) * sms);
+  const int32_t rows = static_cast<int32_t>((p.M + ctas - 1) / ctas);
+  const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(p.M) + rows - 1) / rows);
+  return launch_overlapped(gated_norm_kernel<CH, F32, FP8>, dim3(grid), dim3(threads), 0, stream, p, rows);
+}
+
+template <int CH>
+cudaError_t launch_chunks(const GatedNorm& p, int dev, int sms, cudaStream_t stream) {
   const bool fp8 = p.scales != nullptr;
-  const auto kernel = p.f32 ? (fp8 ? gated_norm_kernel<W, CH, true, true> : gated_norm_kernel<W, CH, true, false>)
-                            : (fp8 ? gated_norm_kernel<W, CH, false, true> : gated_norm_kernel<W, CH, false, false>);
-  return launch_overlapped(kernel, dim3(grid), dim3(32 * kWarps), 0, stream, p);
-}
-
-template <int W>
-cudaError_t launch_warps(const GatedNorm& p, int ch, cudaStream_t stream) {
-  switch (ch) {
-    case 1: return launch_shape<W, 1>(p, stream);
-    case 2: return launch_shape<W, 2>(p, stream);
-    case 3: return launch_shape<W, 3>(p, stream);
-    case 4: return launch_shape<W, 4>(p, stream);
-    default: return launch_shape<W, 5>(p, stream);
-  }
+  return p.f32 ? (fp8 ? launch<CH, true, true>(p, dev, sms, stream) : launch<CH, true, false>(p, dev, sms, stream))
+               : (fp8 ? launch<CH, false, true>(p, dev, sms, stream) : launch<CH, false, false>(p, dev, sms, stream));
 }
 
 }  // namespace
 
 trdq_status launch_gated_norm(const GatedNorm& p, cudaStream_t stream) {
-  const int chunks = p.D / 8;
-  int W = 1;
-  while (W < kWarps && (chunks + 32 * W - 1) / (32 * W) > 5) W *= 2;
-  const int ch = (chunks + 32 * W - 1) / (32 * W);
-  if (ch > 5) return TRDQ_ERR_SHAPE;
-  const cudaError_t e = W == 1 ? launch_warps<1>(p, ch, stream) : W == 2 ? launch_warps<2>(p, ch, stream) : W == 4 ? launch_warps<4>(p, ch, stream) : launch_warps<8>(p, ch, stream);
+  int dev = 0, sms = 148;
+  if (cudaGetDevice(&dev) != cudaSuccess) return TRDQ_ERR_CUDA;
+  cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (row_threads(p.D) > 32 * kRowWarps) return TRDQ_ERR_SHAPE;
+  const cudaError_t e = row_chunks(p.D) == 1 ? launch_chunks<1>(p, dev, sms, stream) : launch_chunks<2>(p, dev, sms, stream);
   return e == cudaSuccess ? TRDQ_OK : TRDQ_ERR_CUDA;
 }
 

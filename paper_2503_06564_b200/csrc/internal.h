@@ -216,7 +216,7 @@ struct GatedNormBackward {
   float eps, alpha;
   bool f32;
 };
-void gated_norm_backward_runs(int32_t M, int32_t rows_per_sample, int32_t* samples, int32_t* runs, int32_t* rows_per_run);
+void gated_norm_backward_runs(int32_t M, int32_t D, int32_t rows_per_sample, int32_t* samples, int32_t* runs, int32_t* rows_per_run);
 trdq_status launch_gated_norm_backward(const GatedNormBackward& p, cudaStream_t stream);
 
 // tensor maps (driver entry point fetched through the runtime; no link-time libcuda dependency)
