@@ -329,6 +329,10 @@ trdq_status launch_gemm_fp8(const Fp8Linear& a, cudaStream_t stream) {
   int dev = 0, sms = 148;
   if (cudaGetDevice(&dev) != cudaSuccess) return TRDQ_ERR_CUDA;
   cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (a.M > 512) {
+    const trdq_status st = launch_gemm_fp8_pair(a, stream);
+    if (st != TRDQ_ERR_SHAPE) return st;
+  }
   if (a.M <= 16) return launch_tokens<16>(a, sms, dev, stream);
   if (a.M <= 32) return launch_tokens<32>(a, sms, dev, stream);
   if (a.M <= 64) return launch_tokens<64>(a, sms, dev, stream);
