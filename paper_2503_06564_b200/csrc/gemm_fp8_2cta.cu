@@ -1,14 +1,25 @@
 // Product of block-scaled e4m3 codes (gemm_fp8.cu has the formula), CTA-PAIR variant for many rows (tcgen05 cta_group::2).
 //
-// Two CTAs of a cluster compute one 256 x BN tile of Y: each loads its own 128 rows of the activation codes and half of the weight tile, one
+// Two CTAs of a cluster compute one 256 x 128 tile of Y: each loads its own 128 rows of the activation codes and half of the weight tile, one
 // thread of the leader issues the MMAs of both.  A k-block of the pipeline is one scale block, so every k-block's sums are complete numbers in an
-// accumulator slot of their own, and the epilogue warps add them up in registers, acc = fma(p, fl(sx sw), acc), while the next k-block is
-// multiplied:
+// accumulator of their own, and drain warps add them up in registers, acc = fma(p, fl(sx sw), acc), while the next k-blocks are multiplied:
 //   warp 0       TMA of both operands (both CTAs)
-//   warp 1       MMAs (leader)
-//   warps 4-11   drain: a thread owns one row and half of the tile's columns; its row scale changes with the k-block, the weight scale with
-//                k-block and 128-column block.  At the end of a tile bias, activation, bf16, staging tile, TMA store.
+//   warp 1       MMAs (leader), four accumulators of 128 columns in turn
+//   warp 2       waits for the accumulators' mbarriers and wakes the drain through hardware barriers
+//   warps 4-19   drain: two sets of eight warps that take every second tile.  A thread owns one row and 64 columns, its scale is one number a
+//                k-block; at the end of a tile bias, activation, bf16, staging tile, TMA store, while the other set adds up the next tile.
 // Synchronisation as in gemm_i8_2cta.cu, with the accumulator barriers per k-block; every wait bounded.
+//
+// What bounds it: operand delivery from L2 (24 KB a CTA and k-block, 11 TB/s over the SMs), close behind it the drain.  Beside MMAs and copies a
+// shared-memory access of another warp is slow, an mbarrier wait that is over takes 70 to 200 clocks, against 256 clocks of MMA and 130 of multiply-adds
+// for a k-block.  So one warp waits for all, and hardware barriers (20 clocks) pass it on; and the scales are requested ahead (the row's line fetched
+// only a k-block before its use, the round trip set the pace: 32768 x 1152 x 4608 219 us in place of 187, 4096 x 1152 x 4608 32 in place of 28).
+// M x N x K, microseconds with one set of drain warps -> two: 4096 x 4608 x 1152 33 -> 28, 2057 x 4624 x 1152 21 -> 18, 16384 x 3456 x 1152 84 -> 73;
+// long reductions 32768 x 1152 x 4608 178 -> 187, 8192 x 4096 x 4096 140 -> 139.
+// Measured and not better: tiles of 256 x 256, which need 2/3 of the operand bytes but leave tensor memory two accumulators and a thread 128 sums
+// (1040 clocks a k-block in place of 512: the hand-over MMA - commit - wait - loads - release - wait is longer than the MMAs of the other accumulator;
+// 32768 x 1152 x 4608 189, 4096 x 1152 x 4608 36, 8192 x 4096 x 4096 131); the same with each 128-column half handed over by itself and sixteen drain
+// warps at once (210, 48, 166: four warps a scheduler, each with the loop's own instructions); 256 x 192 (189, 36, 159); scales through shared memory.
 #include <cuda_bf16.h>
 
 #include "epilogue.cuh"
@@ -20,37 +31,38 @@ namespace trdq {
 namespace {
 
 constexpr int kTileM = 128;  // rows per CTA; the pair covers 256
+constexpr int kTileCh = 128;  // columns: one scale block of the weights
 constexpr int kTileK = 128;  // one scale block
 constexpr int kUmmaK = 32;
 constexpr int kTmemCols = 512;
-constexpr int kDrainWarps = 8;
+constexpr int kAccs = kTmemCols / kTileCh;
+constexpr int kSets = 2;            // of drain warps
+constexpr int kSetWarps = 8;        // 4 lane quarters of tensor memory x 2 column halves
+constexpr int kDrainWarps = kSets * kSetWarps;
+constexpr int kCols = kTileCh / 2;  // of a drain thread
 constexpr int kThreads = 128 + 32 * kDrainWarps;
-constexpr int kSmemBudget = 227 * 1024;
-// Registers: the drain holds up to 128 sums and a double-buffered tensor-memory load a thread, the other warpgroup little.
-constexpr int kRegsLaunch = 168, kRegsDrain = 208, kRegsOther = 80;
+constexpr int kAhead = 4;  // k-blocks that the row scales are brought into L1 before they are used
+// Registers: 640 threads are launched with 96 each; the drain's 64 sums, a tensor-memory load of 16 and its loop need a little more, the others less.
+constexpr int kRegsLaunch = 96, kRegsDrain = 104, kRegsOther = 64;
 static_assert(32 * kDrainWarps * kRegsDrain + 128 * kRegsOther <= kThreads * kRegsLaunch, "register split exceeds the launch's allocation");
-
-template <int BN>
-struct Cfg {
-  static constexpr int kSlotStride = BN == 128 ? 128 : 256;
-  static constexpr int kSlots = kTmemCols / kSlotStride;
-  static constexpr int kABytes = kTileM * kTileK;
-  static constexpr int kBBytes = (BN / 2) * kTileK;  // this CTA's half of the weight tile
-  static constexpr int kStageBytes = kABytes + kBBytes;
-  static constexpr int kOutBytes = kDrainWarps * 4096;  // a 32 x 64 bf16 tile per drain warp
-  static constexpr int kBarrierBytes = 512;
-  static constexpr int kStages = (kSmemBudget - 1024 - kOutBytes - kBarrierBytes) / kStageBytes;
-  static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kOutBytes + kBarrierBytes;
-  static constexpr int kCols = BN / 2;  // of a drain thread
-  static_assert(kStageBytes % 1024 == 0 && kStages >= 4, "stages");
-  static_assert((2 * kStages + 2 * kSlots) * 8 + 4 <= kBarrierBytes, "barriers");
-};
+constexpr int kABytes = kTileM * kTileK;
+constexpr int kBBytes = (kTileCh / 2) * kTileK;  // this CTA's half of the weight tile
+constexpr int kStageBytes = kABytes + kBBytes;
+constexpr int kOutBytes = kDrainWarps * 4096;  // a 32 x 64 bf16 tile per drain warp
+constexpr int kBiasBytes = kDrainWarps * kCols * 4;
+constexpr int kBarrierBytes = 512;
+constexpr int kStages = (227 * 1024 - 1024 - kOutBytes - kBiasBytes - kBarrierBytes) / kStageBytes;
+constexpr int kOutOff = kStages * kStageBytes;
+constexpr int kBiasOff = kOutOff + kOutBytes;
+constexpr int kBarOff = kBiasOff + kBiasBytes;
+constexpr int kSmemBytes = 1024 + kBarOff + kBarrierBytes;
+static_assert(kStageBytes % 1024 == 0, "stage tiles must stay 1024-byte aligned");
+static_assert((2 * kStages + 2 * kAccs) * 8 + 4 <= kBarrierBytes, "barriers");
 
 struct alignas(64) Fp8PairParams {
-  CUtensorMap tmap_a;      // activation codes, box 128 B x 128 rows
-  CUtensorMap tmap_b;      // weight codes, box 128 B x BN/2 rows
-  CUtensorMap tmap_out;    // bf16 output, box 64 x 32, 128-byte swizzle
-  CUtensorMap tmap_out32;  // box 32 x 32, 64-byte swizzle: the odd chunk of BN = 192
+  CUtensorMap tmap_a;    // activation codes, box 128 B x 128 rows
+  CUtensorMap tmap_b;    // weight codes, box 128 B x 64 rows
+  CUtensorMap tmap_out;  // bf16 output, box 64 x 32, 128-byte swizzle
   const float* sx;
   const float* sw;
   const __nv_bfloat16* bias;
@@ -68,21 +80,19 @@ __device__ __forceinline__ void umma_fp8_pair(uint32_t d_tmem, uint64_t a_desc, 
       : "memory");
 }
 // kind::f8f6f4: fp32 D, e4m3 A and B (format 0), both K-major, M = 256.
-__host__ __device__ constexpr uint32_t umma_idesc_e4m3_pair(int n) {
-  return (1u << 4) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(256 >> 4) << 24);
-}
+constexpr uint32_t kIdesc = (1u << 4) | (static_cast<uint32_t>(kTileCh >> 3) << 17) | (static_cast<uint32_t>(256 >> 4) << 24);
 
 struct Tile {
   int m0, n0;
 };
 // Bands of `band` row tiles, column block by column block inside a band: the clusters that run at once cover a rectangle and share panels in L2.
-__device__ __forceinline__ Tile tile_at(const Fp8PairParams& p, int tile, int bn) {
+__device__ __forceinline__ Tile tile_at(const Fp8PairParams& p, int tile) {
   const int per_band = p.band * p.tiles_n;
   const int b = tile / per_band;
   const int r = tile - b * per_band;
   const int rows = min(p.band, p.tiles_m - b * p.band);
   const int nt = r / rows;
-  return Tile{(b * p.band + (r - nt * rows)) * 2 * kTileM, nt * bn};
+  return Tile{(b * p.band + (r - nt * rows)) * 2 * kTileM, nt * kTileCh};
 }
 
 struct Ring {
@@ -103,19 +113,33 @@ __device__ __forceinline__ void tmem_wait_ld_regs(uint32_t (&r)[16]) {
   for (int i = 0; i < 16; ++i) asm volatile("" : "+r"(r[i]));
 }
 
-template <int BN, bool ACT>
+// Hardware barriers between the warp that waits for the accumulators and the drain, one per accumulator and set.  None is arrived at again before all
+// have passed it: the next arrival follows the accumulator's next MMAs, and those its release.
+constexpr int kMeet = 32 + 32 * kSetWarps;
+__device__ __forceinline__ void wake_arrive(int acc, int set) { asm volatile("bar.arrive %0, %1;" ::"r"(1 + set * kAccs + acc), "n"(kMeet) : "memory"); }
+__device__ __forceinline__ void wake_wait(int acc, int set) { asm volatile("bar.sync %0, %1;" ::"r"(1 + set * kAccs + acc), "n"(kMeet) : "memory"); }
+
+// Lane and drain warp, read anew from the hardware: not kept in registers from one use to the next.
+struct DrainPlace {
+  int lane, dw;
+};
+__device__ __forceinline__ DrainPlace drain_place() {
+  uint32_t tid;
+  asm volatile("mov.u32 %0, %%tid.x;" : "=r"(tid));
+  return DrainPlace{static_cast<int>(tid & 31), static_cast<int>(tid >> 5) - 4};
+}
+
+template <bool ACT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp8_pair_kernel(const __grid_constant__ Fp8PairParams p) {
-  using C = Cfg<BN>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem = smem_raw + (smem_base - smem_u32(smem_raw));
-  const uint32_t out_base = smem_base + C::kStages * C::kStageBytes;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::kStages * C::kStageBytes + C::kOutBytes);
-  const uint32_t bar_full = smem_u32(bars);               // [kStages] used in the leader: both CTAs' tiles landed
-  const uint32_t bar_empty = bar_full + 8 * C::kStages;   // [kStages] each CTA's own: the MMAs have read the stage
-  const uint32_t bar_tfull = bar_empty + 8 * C::kStages;  // [kSlots]  each CTA's own: the k-block's sums are complete
-  const uint32_t bar_tempty = bar_tfull + 8 * C::kSlots;  // [kSlots]  used in the leader: both CTAs have read them
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * C::kStages + 2 * C::kSlots);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kBarOff);
+  const uint32_t bar_full = smem_u32(bars);            // [kStages] used in the leader: both CTAs' tiles landed
+  const uint32_t bar_empty = bar_full + 8 * kStages;   // [kStages] each CTA's own: the MMAs have read the stage
+  const uint32_t bar_tfull = bar_empty + 8 * kStages;  // [kAccs]   each CTA's own: the k-block's sums are complete
+  const uint32_t bar_tempty = bar_tfull + 8 * kAccs;   // [kAccs]   used in the leader: both CTAs have read them
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kStages + 2 * kAccs);
 
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
@@ -126,19 +150,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
   const int total_tiles = p.tiles_m * p.tiles_n;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < C::kStages; ++s) {
+    for (int s = 0; s < kStages; ++s) {
       mbar_init(bar_full + 8 * s, 2);   // one arrive.expect_tx from each CTA's producer
       mbar_init(bar_empty + 8 * s, 1);  // one multicast commit
     }
-    for (int a = 0; a < C::kSlots; ++a) {
+    for (int a = 0; a < kAccs; ++a) {
       mbar_init(bar_tfull + 8 * a, 1);
-      mbar_init(bar_tempty + 8 * a, 2 * kDrainWarps);
+      mbar_init(bar_tempty + 8 * a, 2 * kSetWarps);  // a set's warps of both CTAs
     }
     fence_mbar_init();
     prefetch_tensormap(&p.tmap_a);
     prefetch_tensormap(&p.tmap_b);
     prefetch_tensormap(&p.tmap_out);
-    if (BN == 192) prefetch_tensormap(&p.tmap_out32);
   }
   if (warp == 2) {
     tmem_alloc_pair(smem_u32(tmem_slot), kTmemCols);
@@ -155,141 +178,164 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
   if (warp >= 4) {
     // ------------------------------------------------------------------- drain (both CTAs, own 128 rows)
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsDrain));
-    const int dw = warp - 4;
-    const int q = dw & 3;  // = warp % 4: the lane quarter of tensor memory this warp may read
-    const int half = dw >> 2;
-    const uint32_t my_stage = out_base + dw * 4096;
-    const uint32_t t_lane = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + half * C::kCols;
+    const int set = (warp - 4) / kSetWarps;
+    // what a tile's beginning and end need is worked out there: kept through the loop it would not fit the registers
+    const uint32_t t_lane = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16) + ((warp - 4) / 4 % 2) * kCols;  // warp % 4: the lane quarter it may read
     const uint32_t leader_tempty = map_to_cta(bar_tempty, 0);
-    const int last_block = (p.N - 1) / kTileK;
-    BoundedWaiter w(p.status, kStatusTimeoutEpilogue);
-    Ring slot;
-    for (int tile = cluster_id; tile < total_tiles; tile += num_clusters) {
-      const Tile t = tile_at(p, tile, BN);
-      const int m0 = t.m0 + static_cast<int>(rank) * kTileM + q * 32;
-      const int c0 = t.n0 + half * C::kCols;
-      const bool row_in = m0 + lane < p.M;
-      const float* sxp = p.sx + (row_in ? m0 + lane : 0);
-      // weight scales of the thread's columns: one 128-column block, or (BN = 192) two
-      const float* swp = p.sw + static_cast<int64_t>(min(c0 / kTileK, last_block)) * p.num_kb;
-      const float* swp2 = p.sw + static_cast<int64_t>(min((c0 + C::kCols - 1) / kTileK, last_block)) * p.num_kb;
-      float2 acc[C::kCols / 2];
+    // Scales of the next k-block, requested while this one is added up: from L1, where the row's was brought kAhead k-blocks before (it is of another line
+    // in every k-block; the registers for that many would not fit).  The first of a tile are requested before the end of the set's tile before.
+    float qx = 0.0f, qw = 0.0f;
+    const float *sxp = nullptr, *swp = nullptr;
+    auto scales_of = [&](int tile) {
+      const DrainPlace d = drain_place();
+      const Tile t = tile_at(p, tile);
+      const int row = t.m0 + static_cast<int>(cluster_ctarank()) * kTileM + (d.dw & 3) * 32 + d.lane;
+      sxp = p.sx + (row < p.M ? row : 0);
+      swp = p.sw + static_cast<int64_t>(t.n0 / kTileCh) * p.num_kb;
+    };
+    auto request = [&](int kb) {
+      if (kb >= p.num_kb) return;
+      qx = __ldg(sxp + static_cast<int64_t>(kb) * p.M);
+      qw = __ldg(swp + kb);
+      if (kb + kAhead < p.num_kb) asm volatile("prefetch.global.L1 [%0];" ::"l"(sxp + static_cast<int64_t>(kb + kAhead) * p.M));
+    };
+    const int first = cluster_id + set * num_clusters;
+    if (first < total_tiles) {
+      scales_of(first);
+      request(0);
+    }
+    int acc_idx = set * (p.num_kb % kAccs);                        // accumulator of the next k-block
+    const int passed_over = (kSets - 1) * (p.num_kb % kAccs);      // those of the other set's tile between two of this one
+    for (int tile = first; tile < total_tiles; tile += kSets * num_clusters) {
+      float2 acc[kCols / 2];
 #pragma unroll
-      for (int j = 0; j < C::kCols / 2; ++j) acc[j] = make_float2(0.0f, 0.0f);
-      float sx = __ldg(sxp), sw = __ldg(swp), sw2 = BN == 192 ? __ldg(swp2) : 0.0f;
+      for (int j = 0; j < kCols / 2; ++j) acc[j] = make_float2(0.0f, 0.0f);
 #pragma unroll 1
       for (int kb = 0; kb < p.num_kb; ++kb) {
-        const float s0 = __fmul_rn(sx, sw), s1 = BN == 192 ? __fmul_rn(sx, sw2) : s0;
-        if (kb + 1 < p.num_kb) {
-          sxp += p.M;
-          sx = __ldg(sxp);
-          sw = __ldg(swp + kb + 1);
-          if (BN == 192) sw2 = __ldg(swp2 + kb + 1);
-        }
-        w.wait(bar_tfull + 8 * slot.idx, slot.phase);
-        __syncwarp();
+        const float scale = __fmul_rn(qx, qw);
+        const float2 s2 = make_float2(scale, scale);
+        request(kb + 1);
+        wake_wait(acc_idx, set);
         tc_fence_after();
-        const uint32_t t_row = t_lane + slot.idx * C::kSlotStride;
-        uint32_t r[2][16];
-        tmem_ld_32x16(t_row, r[0]);
+        const uint32_t t_row = t_lane + acc_idx * kTileCh;
 #pragma unroll
-        for (int c = 0; c < C::kCols / 16; ++c) {
-          tmem_wait_ld_regs(r[c & 1]);
-          if (c + 1 < C::kCols / 16) {
-            tmem_ld_32x16(t_row + (c + 1) * 16, r[(c + 1) & 1]);
-          } else {
+        for (int c = 0; c < kCols / 16; ++c) {
+          uint32_t r[16];
+          tmem_ld_32x16(t_row + c * 16, r);
+          tmem_wait_ld_regs(r);
+          if (c + 1 == kCols / 16) {
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_remote_arrive(leader_tempty + 8 * slot.idx);
+            if (lane == 0) mbar_remote_arrive(leader_tempty + 8 * acc_idx);
+            acc_idx = (acc_idx + 1) % kAccs;
           }
-          const float s = BN == 192 && (c0 + 16 * c) / kTileK != c0 / kTileK ? s1 : s0;
-          const float2 s2 = make_float2(s, s);
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            acc[c * 8 + j] = __ffma2_rn(make_float2(__uint_as_float(r[c & 1][2 * j]), __uint_as_float(r[c & 1][2 * j + 1])), s2, acc[c * 8 + j]);
+            acc[c * 8 + j] = __ffma2_rn(make_float2(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1])), s2, acc[c * 8 + j]);
         }
-        slot.advance(C::kSlots);
       }
-      // bias, activation, bf16; 64 columns per store (32 in the odd chunk of BN = 192)
+      acc_idx = (acc_idx + passed_over) % kAccs;
+      if (tile + kSets * num_clusters < total_tiles) {
+        scales_of(tile + kSets * num_clusters);
+        request(0);
+      }
+      // bias, activation, bf16
+      const DrainPlace d = drain_place();
+      const Tile t = tile_at(p, tile);
+      const int m0 = t.m0 + static_cast<int>(cluster_ctarank()) * kTileM + (d.dw & 3) * 32;
+      const int c0 = t.n0 + (d.dw / 4 % 2) * kCols;
+      const uint32_t my_stage = smem_base + kOutOff + d.dw * 4096;
+      float* const my_bias = reinterpret_cast<float*>(smem + kBiasOff) + d.dw * kCols;
+      {
+        const int n = c0 + 2 * d.lane;
+        const uint32_t b = p.bias && n < p.N ? __ldg(reinterpret_cast<const uint32_t*>(p.bias + n)) : 0u;
+        *reinterpret_cast<float2*>(my_bias + 2 * d.lane) = make_float2(__uint_as_float(b << 16), __uint_as_float(b & 0xFFFF0000u));
+      }
+      if (d.lane == 0) bulk_wait_group_read<0>();  // the previous store has finished reading the staging tile
+      __syncwarp();
 #pragma unroll
-      for (int c = 0; c < C::kCols; c += 64) {
-        const bool wide = c + 64 <= C::kCols;
-        if (lane == 0) bulk_wait_group_read<0>();  // the previous store has finished reading the staging tile
-        __syncwarp();
+      for (int v = 0; v < 8; ++v) {
+        const float4 ba = *reinterpret_cast<const float4*>(my_bias + 8 * v), bb = *reinterpret_cast<const float4*>(my_bias + 8 * v + 4);
+        const float2 bias[4] = {make_float2(ba.x, ba.y), make_float2(ba.z, ba.w), make_float2(bb.x, bb.y), make_float2(bb.z, bb.w)};
+        uint32_t packed[4];
 #pragma unroll
-        for (int v = 0; v < (wide ? 8 : 4); ++v) {
-          const int n = c0 + c + 8 * v;
-          uint2 b[2] = {make_uint2(0u, 0u), make_uint2(0u, 0u)};
-          if (p.bias && n < p.N) {
-            b[0] = __ldg(reinterpret_cast<const uint2*>(p.bias + n));
-            b[1] = __ldg(reinterpret_cast<const uint2*>(p.bias + n) + 1);
-          }
-          uint32_t packed[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t bw = j & 1 ? b[j / 2].y : b[j / 2].x;
-            float2 y = __fadd2_rn(acc[(c + 8 * v) / 2 + j], make_float2(__uint_as_float(bw << 16), __uint_as_float(bw & 0xFFFF0000u)));
-            if constexpr (ACT) y = gelu_tanh2<false>(y);
-            packed[j] = pack_bf16(y);
-          }
-          const uint32_t at = wide ? my_stage + lane * 128 + ((v ^ (lane & 7)) << 4) : my_stage + lane * 64 + ((v ^ ((lane >> 1) & 3)) << 4);
-          st_shared_v4(at, packed[0], packed[1], packed[2], packed[3]);
+        for (int j = 0; j < 4; ++j) {
+          float2 y = __fadd2_rn(acc[4 * v + j], bias[j]);
+          if constexpr (ACT) y = gelu_tanh2<false>(y);
+          packed[j] = pack_bf16(y);
         }
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0 && m0 < p.M && c0 + c < p.N) {
-          tma_store_2d(wide ? &p.tmap_out : &p.tmap_out32, c0 + c, m0, my_stage);  // rows >= M and columns >= N are clipped
-          bulk_commit_group();
-        }
+        st_shared_v4(my_stage + d.lane * 128 + ((v ^ (d.lane & 7)) << 4), packed[0], packed[1], packed[2], packed[3]);
+      }
+      fence_proxy_async_smem();
+      __syncwarp();  // (the biases have been read, too)
+      if (d.lane == 0 && m0 < p.M && c0 < p.N) {
+        tma_store_2d(&p.tmap_out, c0, m0, my_stage);  // rows >= M and columns >= N are clipped
+        bulk_commit_group();
       }
     }
-    if (lane == 0) bulk_wait_group_read<0>();
-    w.settle();
+    if (lane == 0) bulk_wait_group_read<0>();  // the staging tiles have been read; the stores complete before the grid does
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
     if (warp == 0) {
+      // ------------------------------------------------------------------- TMA producer (both CTAs)
       if (elect_one()) {
         BoundedWaiter w(p.status, kStatusTimeoutProducer);
         const uint32_t leader_full = map_to_cta(bar_full, 0);
         Ring st;
         for (int tile = cluster_id; tile < total_tiles; tile += num_clusters) {
-          const Tile t = tile_at(p, tile, BN);
+          const Tile t = tile_at(p, tile);
           for (int kb = 0; kb < p.num_kb; ++kb) {
             w.wait(bar_empty + 8 * st.idx, st.phase ^ 1);
-            const uint32_t a_dst = smem_base + st.idx * C::kStageBytes, full = leader_full + 8 * st.idx;
-            mbar_remote_arrive_expect_tx(full, C::kStageBytes);
+            const uint32_t a_dst = smem_base + st.idx * kStageBytes, full = leader_full + 8 * st.idx;
+            mbar_remote_arrive_expect_tx(full, kStageBytes);
             tma_load_2d_pair(a_dst, &p.tmap_a, kb * kTileK, t.m0 + rank * kTileM, full);
-            tma_load_2d_pair(a_dst + C::kABytes, &p.tmap_b, kb * kTileK, t.n0 + rank * (BN / 2), full);
-            st.advance(C::kStages);
+            tma_load_2d_pair(a_dst + kABytes, &p.tmap_b, kb * kTileK, t.n0 + rank * (kTileCh / 2), full);
+            st.advance(kStages);
           }
         }
         w.settle();
       }
+      __syncwarp();
     } else if (warp == 1) {
+      // ------------------------------------------------------------------- MMA issuer (leader only)
       if (leader && elect_one()) {
         BoundedWaiter w(p.status, kStatusTimeoutMma);
-        constexpr uint32_t idesc = umma_idesc_e4m3_pair(BN);
-        Ring st, slot;
+        Ring st, acc;
         for (int tile = cluster_id; tile < total_tiles; tile += num_clusters) {
           for (int kb = 0; kb < p.num_kb; ++kb) {
-            w.wait(bar_tempty + 8 * slot.idx, slot.phase ^ 1);
+            w.wait(bar_tempty + 8 * acc.idx, acc.phase ^ 1);
             w.wait(bar_full + 8 * st.idx, st.phase);
             tc_fence_after();
-            const uint32_t a_addr = smem_base + st.idx * C::kStageBytes;
-            const uint64_t a_desc = umma_desc_k_sw128(a_addr), b_desc = umma_desc_k_sw128(a_addr + C::kABytes);
+            const uint32_t a_addr = smem_base + st.idx * kStageBytes;
+            const uint64_t a_desc = umma_desc_k_sw128(a_addr), b_desc = umma_desc_k_sw128(a_addr + kABytes);
 #pragma unroll
-            for (int k = 0; k < kTileK / kUmmaK; ++k)
-              umma_fp8_pair(tmem_base + slot.idx * C::kSlotStride, a_desc + 2 * k, b_desc + 2 * k, idesc, k != 0 ? 1u : 0u);
+            for (int k = 0; k < kTileK / kUmmaK; ++k) umma_fp8_pair(tmem_base + acc.idx * kTileCh, a_desc + 2 * k, b_desc + 2 * k, kIdesc, k != 0 ? 1u : 0u);
             umma_commit_pair(bar_empty + 8 * st.idx);
-            umma_commit_pair(bar_tfull + 8 * slot.idx);
-            st.advance(C::kStages);
-            slot.advance(C::kSlots);
+            umma_commit_pair(bar_tfull + 8 * acc.idx);
+            st.advance(kStages);
+            acc.advance(kAccs);
           }
         }
         w.settle();
       }
+      __syncwarp();
+    } else if (warp == 2) {
+      // ------------------------------------------------------------------- an accumulator is complete: wake the drain (one lane asks; 32 would be 32 accesses)
+      BoundedWaiter w(p.status, kStatusTimeoutEpilogue);
+      Ring acc;
+      int set = 0;
+      for (int tile = cluster_id; tile < total_tiles; tile += num_clusters) {
+        for (int kb = 0; kb < p.num_kb; ++kb) {
+          if (lane == 0) w.wait(bar_tfull + 8 * acc.idx, acc.phase);
+          __syncwarp();
+          wake_arrive(acc.idx, set);
+          acc.advance(kAccs);
+        }
+        set ^= 1;
+      }
+      w.settle();
+      __syncwarp();
     }
-    __syncwarp();
   }
 
   // Neither CTA may release its shared or tensor memory while the other's MMAs or copies can still touch it.
@@ -303,33 +349,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
 }
 
 // Clusters of two CTAs that can be resident at once; 0: the kernel cannot run here.
-template <int BN>
 int resident_clusters(int dev) {
   static PerDevice<int> cached;
   int known = cached.get(dev);
   if (known != 0) return known > 0 ? known : 0;
-  using C = Cfg<BN>;
   bool ok = true;
-  for (const auto kernel : {gemm_fp8_pair_kernel<BN, false>, gemm_fp8_pair_kernel<BN, true>}) {
+  for (const auto kernel : {gemm_fp8_pair_kernel<false>, gemm_fp8_pair_kernel<true>}) {
     cudaFuncAttributes attr;
     // the register split draws on what the launch allocates
     ok = ok && cudaFuncGetAttributes(&attr, kernel) == cudaSuccess && attr.numRegs == kRegsLaunch &&
-         cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes) == cudaSuccess;
+         cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) == cudaSuccess;
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2);
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = C::kSmemBytes;
+  cfg.dynamicSmemBytes = kSmemBytes;
   int n = 0;
-  ok = ok && cudaOccupancyMaxActiveClusters(&n, gemm_fp8_pair_kernel<BN, false>, &cfg) == cudaSuccess && n > 0;
+  ok = ok && cudaOccupancyMaxActiveClusters(&n, gemm_fp8_pair_kernel<false>, &cfg) == cudaSuccess && n > 0;
   if (!ok) cudaGetLastError();
   cached.set(dev, ok ? n : -1);
   return ok ? n : 0;
-}
-
-template <int BN, bool ACT>
-cudaError_t launch_pair(const Fp8PairParams& p, int clusters, cudaStream_t stream) {
-  return launch_overlapped(gemm_fp8_pair_kernel<BN, ACT>, dim3(2 * clusters), dim3(kThreads), Cfg<BN>::kSmemBytes, stream, p);
 }
 
 }  // namespace
@@ -337,22 +376,12 @@ cudaError_t launch_pair(const Fp8PairParams& p, int clusters, cudaStream_t strea
 trdq_status launch_gemm_fp8_pair(const Fp8Linear& a, cudaStream_t stream) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return TRDQ_ERR_CUDA;
-  const int64_t tiles_m = (static_cast<int64_t>(a.M) + 2 * kTileM - 1) / (2 * kTileM);
-  int bn = 0, resident = 0;
-  double best = 0.0;
-  for (const int cand : {256, 192, 128}) {
-    const int clusters = cand == 256 ? resident_clusters<256>(dev) : cand == 192 ? resident_clusters<192>(dev) : resident_clusters<128>(dev);
-    if (clusters == 0) continue;
-    const int64_t tiles = tiles_m * ((a.N + cand - 1) / cand);
-    const double cost = static_cast<double>((tiles + clusters - 1) / clusters) * (cand + 16);
-    if (bn == 0 || cost < best) bn = cand, resident = clusters, best = cost;
-  }
-  if (bn == 0) return TRDQ_ERR_SHAPE;
+  const int resident = resident_clusters(dev);
+  if (resident == 0) return TRDQ_ERR_SHAPE;
   Fp8PairParams p;
   trdq_status st = encode_tmap_u8_sw128(&p.tmap_a, a.codes, a.K, a.M, a.K, kTileK, kTileM);
-  if (st == TRDQ_OK) st = encode_tmap_u8_sw128(&p.tmap_b, a.w_codes, a.K, a.N, a.K, kTileK, bn / 2);
-  if (st == TRDQ_OK) st = encode_tmap_2d(&p.tmap_out, a.out, 2, a.N, a.M, static_cast<uint64_t>(a.ld) * 2, 64, 32, 128);
-  if (st == TRDQ_OK) st = encode_tmap_2d(&p.tmap_out32, a.out, 2, a.N, a.M, static_cast<uint64_t>(a.ld) * 2, 32, 32, 64);
+  if (st == TRDQ_OK) st = encode_tmap_u8_sw128(&p.tmap_b, a.w_codes, a.K, a.N, a.K, kTileK, kTileCh / 2);
+  if (st == TRDQ_OK) st = encode_tmap_2d(&p.tmap_out, a.out, 2, a.N, a.M, static_cast<uint64_t>(a.ld) * 2, kCols, 32, 128);
   if (st != TRDQ_OK) return st;
   p.sx = a.scales;
   p.sw = a.w_scales;
@@ -360,17 +389,17 @@ trdq_status launch_gemm_fp8_pair(const Fp8Linear& a, cudaStream_t stream) {
   p.M = a.M;
   p.N = a.N;
   p.num_kb = a.K / kTileK;
+  const int64_t tiles_m = (static_cast<int64_t>(a.M) + 2 * kTileM - 1) / (2 * kTileM);
   p.tiles_m = static_cast<int32_t>(tiles_m);
-  p.tiles_n = (a.N + bn - 1) / bn;
+  p.tiles_n = (a.N + kTileCh - 1) / kTileCh;
   const int64_t total = tiles_m * p.tiles_n;
   if (total > 0x3FFFFFFF) return TRDQ_ERR_SHAPE;
   p.band = tiles_m >= 32 ? 4 : p.tiles_m;
   p.status = device_status_word();
   if (!p.status) return TRDQ_ERR_CUDA;
   const int clusters = static_cast<int>(total < resident ? total : resident);
-  const cudaError_t e = bn == 256   ? (a.act ? launch_pair<256, true>(p, clusters, stream) : launch_pair<256, false>(p, clusters, stream))
-                        : bn == 192 ? (a.act ? launch_pair<192, true>(p, clusters, stream) : launch_pair<192, false>(p, clusters, stream))
-                                    : (a.act ? launch_pair<128, true>(p, clusters, stream) : launch_pair<128, false>(p, clusters, stream));
+  const cudaError_t e = launch_overlapped(a.act ? gemm_fp8_pair_kernel<true> : gemm_fp8_pair_kernel<false>, dim3(2 * clusters), dim3(kThreads), kSmemBytes,
+                                          stream, p);
   return e == cudaSuccess ? TRDQ_OK : TRDQ_ERR_CUDA;
 }
 

@@ -1,5 +1,5 @@
-// Thin inline-PTX wrappers for kernels of CTA clusters: the peer's shared memory and barriers, and the cta_group::2 forms of the TMA
-// loads, the tensor-memory allocation and the commit.
+// Thin inline-PTX wrappers for kernels of CTA clusters: the peer's shared memory and barriers, the cta_group::2 forms of the TMA
+// loads, the tensor-memory allocation and the commit; and small asynchronous copies counted on a barrier.
 #pragma once
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -47,6 +47,15 @@ __device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
                "h"(static_cast<uint16_t>(3))
                : "memory");
+}
+
+// 4 bytes global -> shared, asynchronously; `bytes` = 0 writes a zero and reads nothing.
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, uint32_t bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+// Arrives on the barrier (as one of its expected arrivals) when this thread's cp.async copies so far have landed.
+__device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }
 
 }  // namespace trdq
