@@ -348,8 +348,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
   }
 }
 
+}  // namespace
+
 // Clusters of two CTAs that can be resident at once; 0: the kernel cannot run here.
-int resident_clusters(int dev) {
+int fp8_pair_clusters(int dev) {
   static PerDevice<int> cached;
   int known = cached.get(dev);
   if (known != 0) return known > 0 ? known : 0;
@@ -371,12 +373,10 @@ int resident_clusters(int dev) {
   return ok ? n : 0;
 }
 
-}  // namespace
-
 trdq_status launch_gemm_fp8_pair(const Fp8Linear& a, cudaStream_t stream) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return TRDQ_ERR_CUDA;
-  const int resident = resident_clusters(dev);
+  const int resident = fp8_pair_clusters(dev);
   if (resident == 0) return TRDQ_ERR_SHAPE;
   Fp8PairParams p;
   trdq_status st = encode_tmap_u8_sw128(&p.tmap_a, a.codes, a.K, a.M, a.K, kTileK, kTileM);
