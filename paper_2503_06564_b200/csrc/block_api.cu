@@ -158,9 +158,10 @@ trdq_status trdq_gated_norm_backward_workspace(const trdq_gated_norm_op* op, uin
   if (op->M < 0 || op->D <= 0 || op->D % 8 != 0 || op->D > kMostChannels || op->rows_per_sample < 1) return TRDQ_ERR_SHAPE;
   *bytes = 0;
   if (op->M == 0) return TRDQ_OK;
-  int32_t samples, runs, rows;
-  gated_norm_backward_runs(op->M, op->D, op->rows_per_sample, &samples, &runs, &rows);
-  *bytes = 3ull * static_cast<uint64_t>(samples) * static_cast<uint64_t>(runs) * static_cast<uint64_t>(op->D) * sizeof(float);
+  int32_t rows;
+  int64_t entries;
+  gated_norm_backward_runs(op->M, op->D, op->stream_f32 != 0, op->rows_per_sample, &rows, &entries);
+  *bytes = 3ull * static_cast<uint64_t>(entries) * static_cast<uint64_t>(op->D) * sizeof(float);
   return TRDQ_OK;
 }
 
@@ -188,7 +189,9 @@ trdq_status trdq_gated_norm_backward(const trdq_gated_norm_op* op, const void* d
   if (st != TRDQ_OK) return st;
   if (dX && dX == dR && lddx != lddr && op->M > 1) return TRDQ_ERR_SHAPE;
   GatedNormBackward p;
-  gated_norm_backward_runs(op->M, op->D, op->rows_per_sample, &p.samples, &p.runs, &p.rows_per_run);
+  // without modulation the rows are one sample, which joins faster and needs no more workspace
+  p.rows_per_sample = op->gate_bf16 || op->shift_bf16 || op->scale_bf16 ? op->rows_per_sample : op->M;
+  gated_norm_backward_runs(op->M, op->D, op->stream_f32 != 0, p.rows_per_sample, &p.rows_per_run, &p.entries);
   if (dgate || dshift || dscale || dweight || dpost_weight) {
     uint64_t need = 0;
     trdq_gated_norm_backward_workspace(op, &need);
@@ -222,7 +225,6 @@ trdq_status trdq_gated_norm_backward(const trdq_gated_norm_op* op, const void* d
   p.workspace = static_cast<float*>(workspace);
   p.M = op->M;
   p.D = op->D;
-  p.rows_per_sample = op->rows_per_sample;
   p.norm = op->norm;
   p.post = op->post_norm;
   p.sample_blocks = 0;

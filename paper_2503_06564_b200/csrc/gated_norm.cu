@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(32 * kRowWarps) gated_norm_kernel(const GatedN
   };
   fetch(rows > 0);
 
-  Chunk gate[CH], gain[CH], shift[CH];  // gate o pw, (1 + scale) o w, shift of this thread's columns
+  Chunk gate[CH], gain[CH], shift[CH];  // gate o pw, (1 + scale) o w, shift of this thread's columns; with the rotation the last two times its vector
   int until = 0;                        // rows from row0 on that these hold for
   const float2 alpha2 = make_float2(p.alpha, p.alpha);
   for (int i = 0; i < rows; ++i) {
@@ -133,6 +133,13 @@ __global__ void __launch_bounds__(32 * kRowWarps) gated_norm_kernel(const GatedN
         if (p.weight) gain[j] = chunk_mul(gain[j], widen(w[j]));
         shift[j] = widen(sh[j]);
         if (!in[j]) shift[j] = none;
+        if constexpr (FP8) {
+          if (p.vec && in[j]) {
+            const Chunk vec = load_vec(p.vec, at[j]);
+            gain[j] = chunk_mul(gain[j], vec);
+            shift[j] = chunk_mul(shift[j], vec);
+          }
+        }
       }
     }
     StreamChunk<F32> x[CH];
@@ -164,10 +171,7 @@ __global__ void __launch_bounds__(32 * kRowWarps) gated_norm_kernel(const GatedN
     for (int j = 0; j < CH; ++j) {
       v[j] = chunk_fma(chunk_scale(v[j], f), gain[j], shift[j]);
       if constexpr (FP8) {
-        if (p.vec) {
-          if (in[j]) v[j] = chunk_mul(v[j], load_vec(p.vec, at[j]));
-          wht128_lanes16(v[j], lane);
-        }
+        if (p.vec) wht128_lanes16(v[j], lane);
         float m = chunk_absmax(v[j]);
 #pragma unroll
         for (int k = 1; k < 16; k <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));

@@ -7,9 +7,10 @@
 //   dw = sum_s (1 + scale_s) o A_s        dpw = sum_s gate_s o C_s
 // (no mean(dn), mean(du) for the root mean square.)  Three column sums per sample therefore give all five parameter gradients.
 //
-// A CTA holds one row at a time, CH chunks of eight channels a thread, and walks down a run of rows of one sample, so that a thread's
-// columns and their running sums stay in its registers.  The runs' sums go to the workspace and are joined by a second kernel in a
-// fixed order: equal inputs give equal gradients.  The statistics are taken again from r and b, which are in registers for the gradient itself.
+// A CTA holds one row at a time, CH chunks of eight channels a thread, and walks down a run of rows, so that a thread's columns and their
+// running sums stay in its registers.  The runs are of equal length, one for each CTA that the SMs hold, and cross the samples: where a sample ends, and at the
+// end of the run, the sums go to the workspace, run c's of sample s to entry c + s (each step along the rows moves to the next run, the
+// next sample or both, so no entry is used twice).  A second kernel joins them in a fixed order: equal inputs give equal gradients.  The statistics are taken again from r and b, which are in registers for the gradient itself.
 // What bounds it: memory, 12 bytes a channel with a bf16 stream.
 #include <algorithm>
 
@@ -19,23 +20,97 @@
 namespace trdq {
 namespace {
 
+constexpr int kJoinWarps = 16;
+
 template <bool F32>
 struct RowInputs {
   StreamChunk<F32> r, dr;
   uint4 b, dh;
 };
 
-template <int CH, bool F32>
-__global__ void __launch_bounds__(32 * kRowWarps) gated_norm_backward_kernel(const GatedNormBackward p) {
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
+__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+// What a thread keeps between rows besides its sums: its columns' two parameters, and the inputs of the next row, which are on their way while this row is
+// computed.  In registers (LOCAL false), or in 16-byte pieces of shared memory that no other thread touches, `step` threads apart (LOCAL true): 96 registers
+// instead of 128, so five warps a scheduler and not four.
+template <bool F32, bool LOCAL>
+struct Kept;
+template <bool F32>
+struct Kept<F32, false> {
+  Chunk gain, gate;
+  RowInputs<F32> next;
+  __device__ __forceinline__ void clear(float4*, int) {
+    next.r.clear();
+    next.dr.clear();
+    next.b = next.dh = zero4();
+  }
+  __device__ __forceinline__ void set_params(const Chunk& a, const Chunk& b) { gain = a, gate = b; }
+  __device__ __forceinline__ Chunk get_gain() const { return gain; }
+  __device__ __forceinline__ Chunk get_gate() const { return gate; }
+  __device__ __forceinline__ void request(const char* r, const char* dr, const char* b, const char* dh) {
+    next.r.load(r);
+    if (dr) next.dr.load(dr);
+    if (b) next.b = *reinterpret_cast<const uint4*>(b);
+    next.dh = *reinterpret_cast<const uint4*>(dh);
+  }
+  __device__ __forceinline__ RowInputs<F32> get() const { return next; }
+};
+template <>
+struct Kept<false, true> {
+  static constexpr int kPieces = 8;  // r, dr, b, dh, two of each parameter
+  float4* mine;
+  int step;
+  __device__ __forceinline__ void clear(float4* at, int threads) {
+    mine = at;
+    step = threads;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) mine[k * step] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  }
+  __device__ __forceinline__ void put(int piece, const Chunk& c) {
+    mine[piece * step] = make_float4(c.p[0].x, c.p[0].y, c.p[1].x, c.p[1].y);
+    mine[(piece + 1) * step] = make_float4(c.p[2].x, c.p[2].y, c.p[3].x, c.p[3].y);
+  }
+  __device__ __forceinline__ Chunk chunk(int piece) const {
+    const float4 a = mine[piece * step], b = mine[(piece + 1) * step];
+    return Chunk{{make_float2(a.x, a.y), make_float2(a.z, a.w), make_float2(b.x, b.y), make_float2(b.z, b.w)}};
+  }
+  __device__ __forceinline__ void set_params(const Chunk& a, const Chunk& b) {
+    put(4, a);
+    put(6, b);
+  }
+  __device__ __forceinline__ Chunk get_gain() const { return chunk(4); }
+  __device__ __forceinline__ Chunk get_gate() const { return chunk(6); }
+  // (the pieces of the row before are in registers by now)
+  __device__ __forceinline__ void request(const char* r, const char* dr, const char* b, const char* dh) {
+    const uint32_t at = smem_u32(mine), by = static_cast<uint32_t>(step) * 16;
+    cp_async16(at, r);
+    if (dr) cp_async16(at + by, dr);
+    if (b) cp_async16(at + 2 * by, b);
+    cp_async16(at + 3 * by, dh);
+  }
+  __device__ __forceinline__ RowInputs<false> get() const {
+    cp_async_wait_all();
+    RowInputs<false> v;
+    v.r.load(mine);
+    v.dr.load(mine + step);
+    v.b = *reinterpret_cast<const uint4*>(mine + 2 * step);
+    v.dh = *reinterpret_cast<const uint4*>(mine + 3 * step);
+    return v;
+  }
+};
+
+constexpr int kLocalThreads = 640;  // of an SM, with LOCAL
+
+template <int CH, bool F32, bool LOCAL>
+__global__ void __launch_bounds__(LOCAL ? kLocalThreads : 32 * kRowWarps, 1) gated_norm_backward_kernel(const GatedNormBackward p) {
+  static_assert(CH == 1 || !LOCAL, "one chunk's room a thread");
+  extern __shared__ float4 local[];
   __shared__ float4 slots[RowSum::kSlots];
   RowSum sums(slots);
   const float inv_d = __fdiv_rn(1.0f, static_cast<float>(p.D));
-  const int64_t s = blockIdx.x / p.runs;
-  const int64_t run = blockIdx.x - s * p.runs;
-  const int64_t sample0 = s * p.rows_per_sample;
-  const int64_t row0 = sample0 + run * p.rows_per_run;
-  const int64_t row1 = min(min(row0 + p.rows_per_run, sample0 + p.rows_per_sample), static_cast<int64_t>(p.M));
-  const int rows = static_cast<int>(row1 > row0 ? row1 - row0 : 0);
+  const int64_t row0 = static_cast<int64_t>(blockIdx.x) * p.rows_per_run;
+  const int rows = static_cast<int>(min(static_cast<int64_t>(p.rows_per_run), p.M - row0));
   griddep_launch_dependents();
   griddep_wait();
 
@@ -44,7 +119,6 @@ __global__ void __launch_bounds__(32 * kRowWarps) gated_norm_backward_kernel(con
   int at[CH];
   const char *r_at[CH], *dr_at[CH], *b_at[CH], *dh_at[CH];
   char *dx_at[CH], *db_at[CH];
-  Chunk gain[CH], gate[CH];  // (1 + scale) o w and gate o pw of this thread's columns
   Chunk A[CH], B[CH], C[CH];
   const Chunk none{{make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)}};
 #pragma unroll
@@ -58,30 +132,15 @@ __global__ void __launch_bounds__(32 * kRowWarps) gated_norm_backward_kernel(con
     dx_at[j] = stream_at(p.dx, row0, p.lddx, at[j], F32);
     db_at[j] = stream_at(p.db, row0, p.lddb, at[j], false);
     A[j] = B[j] = C[j] = none;
-    gain[j] = gate[j] = chunk_shift(none, 1.0f);
-    if (!in[j]) continue;
-    if (p.scale) gain[j] = chunk_shift(widen(load_param(p.scale + s * p.ld_scale, at[j])), 1.0f);
-    if (p.weight) gain[j] = chunk_mul(gain[j], widen(load_param(p.weight, at[j])));
-    if (p.gate) gate[j] = widen(load_param(p.gate + s * p.ld_gate, at[j]));
-    if (p.post_weight) gate[j] = chunk_mul(gate[j], widen(load_param(p.post_weight, at[j])));
   }
 
-  RowInputs<F32> next[CH];
+  Kept<F32, LOCAL> kept[CH];
 #pragma unroll
-  for (int j = 0; j < CH; ++j) {  // what is not loaded (lanes outside the row, inputs that are not there) stays zero
-    next[j].r.clear();
-    next[j].dr.clear();
-    next[j].b = next[j].dh = zero4();
-  }
+  for (int j = 0; j < CH; ++j) kept[j].clear(local + threadIdx.x, blockDim.x);  // what is not loaded (lanes outside the row, inputs that are not there) stays zero
   auto fetch = [&](bool valid) {
 #pragma unroll
     for (int j = 0; j < CH; ++j) {
-      if (valid && in[j]) {
-        next[j].r.load(r_at[j]);
-        if (p.dr) next[j].dr.load(dr_at[j]);
-        if (p.b) next[j].b = *reinterpret_cast<const uint4*>(b_at[j]);
-        next[j].dh = *reinterpret_cast<const uint4*>(dh_at[j]);
-      }
+      if (valid && in[j]) kept[j].request(r_at[j], p.dr ? dr_at[j] : nullptr, p.b ? b_at[j] : nullptr, dh_at[j]);
       r_at[j] += p.ldr * kBytes;
       dr_at[j] += p.lddr * kBytes;
       b_at[j] += p.ldb * 2;
@@ -89,15 +148,55 @@ __global__ void __launch_bounds__(32 * kRowWarps) gated_norm_backward_kernel(con
     }
   };
   fetch(rows > 0);
+  int64_t s = row0 / p.rows_per_sample;                                                               // the sample of the row at hand
+  int until = static_cast<int>(min((s + 1) * p.rows_per_sample - row0, static_cast<int64_t>(rows)));  // the run's row it ends at
+  auto begin = [&]() {
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+      Chunk gain = chunk_shift(none, 1.0f), gate = gain;  // (1 + scale) o w and gate o pw of this thread's columns
+      if (in[j]) {
+        if (p.scale) gain = chunk_shift(widen(load_param(p.scale + s * p.ld_scale, at[j])), 1.0f);
+        if (p.weight) gain = chunk_mul(gain, widen(load_param(p.weight, at[j])));
+        if (p.gate) gate = widen(load_param(p.gate + s * p.ld_gate, at[j]));
+        if (p.post_weight) gate = chunk_mul(gate, widen(load_param(p.post_weight, at[j])));
+      }
+      kept[j].set_params(gain, gate);
+    }
+  };
+  auto flush = [&]() {
+    const int64_t plane = static_cast<int64_t>(p.entries) * p.D;
+    auto put = [](float* to, const Chunk& v) {
+      reinterpret_cast<float4*>(to)[0] = make_float4(v.p[0].x, v.p[0].y, v.p[1].x, v.p[1].y);
+      reinterpret_cast<float4*>(to)[1] = make_float4(v.p[2].x, v.p[2].y, v.p[3].x, v.p[3].y);
+    };
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+      if (in[j]) {
+        float* const to = p.workspace + (blockIdx.x + s) * p.D + 8 * at[j];
+        if (p.dscale || p.dweight) put(to, A[j]);
+        if (p.dshift) put(to + plane, B[j]);
+        if (p.dgate || p.dpost_weight) put(to + 2 * plane, C[j]);
+      }
+      A[j] = B[j] = C[j] = none;
+    }
+  };
+  begin();
   const float2 alpha2 = make_float2(p.alpha, p.alpha);
   for (int row = 0; row < rows; ++row) {
+    if (row == until) {
+      flush();
+      ++s;
+      until = static_cast<int>(min(static_cast<int64_t>(until) + p.rows_per_sample, static_cast<int64_t>(rows)));
+      begin();
+    }
     Chunk n[CH], m[CH], dh[CH], dR[CH];
 #pragma unroll
     for (int j = 0; j < CH; ++j) {
-      n[j] = next[j].r.value();
-      m[j] = widen(next[j].b);
-      dh[j] = widen(next[j].dh);
-      dR[j] = next[j].dr.value();
+      const RowInputs<F32> now = kept[j].get();
+      n[j] = now.r.value();
+      m[j] = widen(now.b);
+      dh[j] = widen(now.dh);
+      dR[j] = now.dr.value();
     }
     fetch(row + 1 < rows);
 
@@ -116,7 +215,7 @@ __global__ void __launch_bounds__(32 * kRowWarps) gated_norm_backward_kernel(con
 #pragma unroll
       for (int i = 0; i < 4; ++i) B[j].p[i] = __fadd2_rn(B[j].p[i], dh[j].p[i]);
       A[j] = chunk_fma(dh[j], n[j], A[j]);
-      dn[j] = chunk_mul(dh[j], gain[j]);
+      dn[j] = chunk_mul(dh[j], kept[j].get_gain());
       t = __fadd2_rn(t, make_float2(chunk_dot(dn[j], n[j]), chunk_sum(dn[j])));
     }
     t = sums.two(t);
@@ -129,7 +228,7 @@ __global__ void __launch_bounds__(32 * kRowWarps) gated_norm_backward_kernel(con
       for (int i = 0; i < 4; ++i)
         dR[j].p[i] = __ffma2_rn(__ffma2_rn(n[j].p[i], along2, __fadd2_rn(dn[j].p[i], mean2)), f2, dR[j].p[i]);
       C[j] = chunk_fma(dR[j], m[j], C[j]);
-      du[j] = chunk_mul(dR[j], gate[j]);
+      du[j] = chunk_mul(dR[j], kept[j].get_gate());
       if (p.dx && in[j]) {
         StreamChunk<F32> o;
         Chunk v;
@@ -162,128 +261,111 @@ __global__ void __launch_bounds__(32 * kRowWarps) gated_norm_backward_kernel(con
     }
   }
 
-  // this run's column sums
-  const int64_t plane = static_cast<int64_t>(gridDim.x) * p.D;
-#pragma unroll
-  for (int j = 0; j < CH; ++j) {
-    if (!in[j]) continue;
-    float* const to = p.workspace + static_cast<int64_t>(blockIdx.x) * p.D + 8 * at[j];
-    auto put = [](float* to, const Chunk& v) {
-      reinterpret_cast<float4*>(to)[0] = make_float4(v.p[0].x, v.p[0].y, v.p[1].x, v.p[1].y);
-      reinterpret_cast<float4*>(to)[1] = make_float4(v.p[2].x, v.p[2].y, v.p[3].x, v.p[3].y);
-    };
-    if (p.dscale || p.dweight) put(to, A[j]);
-    if (p.dshift) put(to + plane, B[j]);
-    if (p.dgate || p.dpost_weight) put(to + 2 * plane, C[j]);
-  }
+  flush();
 }
 
-// Joins the runs, four columns a thread.  blockIdx.x < sample_blocks: the gradients of a sample's parameters; the CTAs behind them: those of the
-// weights.  The blockDim.y groups of a CTA take every blockDim.y-th run, and their sums are added in order.
-__global__ void __launch_bounds__(1024) gated_norm_join_kernel(const GatedNormBackward p) {
-  __shared__ float4 part[3][32][32];
-  const int lane = threadIdx.x, group = threadIdx.y, groups = blockDim.y;
-  const int col = (blockIdx.y * 32 + lane) * 4;
-  const bool in = col < p.D;
-  const int64_t count = static_cast<int64_t>(p.samples) * p.runs;
-  const int64_t plane = count * p.D;
-  const bool weights = blockIdx.x >= static_cast<unsigned>(p.sample_blocks);
-  const int64_t first = weights ? 0 : static_cast<int64_t>(blockIdx.x) * p.runs;
-  const int64_t runs = weights ? count : p.runs;
-  const bool want_a = weights ? p.dweight != nullptr : p.dscale != nullptr, want_b = !weights && p.dshift;
-  const bool want_c = weights ? p.dpost_weight != nullptr : p.dgate != nullptr;
+// Joins the entries of one of the three planes (blockIdx.z), 32 columns a CTA, four a thread.  blockIdx.x < sample_blocks: a sample's gradients, from the
+// entries of the runs that it has rows of; the CTAs behind them: the weights' gradients, from all entries.  The groups of eight threads take every
+// `groups`-th entry; their sums are added in order.  Bound by latency: with 128 columns and all three planes in one CTA the sums of 130 runs of 4096 took 7 us instead of 5.
+__global__ void __launch_bounds__(32 * kJoinWarps) gated_norm_join_kernel(const GatedNormBackward p) {
+  __shared__ float4 part[kJoinWarps][8];
+  const int quad = threadIdx.x & 7, group = threadIdx.x >> 3, groups = blockDim.x >> 3, plane = blockIdx.z;
+  const int col = (blockIdx.y * 8 + quad) * 4;
+  const bool in = col < p.D, weights = blockIdx.x >= static_cast<unsigned>(p.sample_blocks);
+  float* const to = plane == 0 ? (weights ? p.dweight : p.dscale) : plane == 1 ? (weights ? nullptr : p.dshift) : weights ? p.dpost_weight : p.dgate;
+  if (!to) return;
+  const int64_t rps = p.rows_per_sample, rpr = p.rows_per_run;
+  const int64_t sample = weights ? 0 : blockIdx.x, end = min((sample + 1) * rps, static_cast<int64_t>(p.M));
+  const int64_t first = sample * rps / rpr + sample, last = weights ? p.entries - 1 : (end - 1) / rpr + sample;
+  const uint16_t* const factor = !weights ? nullptr : plane == 0 ? p.scale : p.gate;
+  const int64_t ld_factor = plane == 0 ? p.ld_scale : p.ld_gate;
+  const float* const from = p.workspace + plane * p.entries * p.D + col;
   griddep_wait();
   auto four = [](const uint16_t* v) {
     const uint2 w = *reinterpret_cast<const uint2*>(v);
     const float2 a = widen_bf16x2(w.x), b = widen_bf16x2(w.y);
     return make_float4(a.x, a.y, b.x, b.y);
   };
+  const float4 none = make_float4(0.0f, 0.0f, 0.0f, 0.0f), one = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
   auto fma4 = [](const float4& a, const float4& b, const float4& c) {
     return make_float4(__fmaf_rn(a.x, b.x, c.x), __fmaf_rn(a.y, b.y, c.y), __fmaf_rn(a.z, b.z, c.z), __fmaf_rn(a.w, b.w, c.w));
   };
-  const float4 one = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
-  float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f), b = a, c = a;
-  if (in) {
+  const uint16_t* const by = weights ? nullptr : plane == 0 ? p.weight : plane == 2 ? p.post_weight : nullptr;
+  const float4 after = by && in ? four(by + col) : one;
+  float4 sum = none;
+  if (in && (!weights || rps >= p.M)) {
+    float4 k = one;
+    if (factor) k = plane == 0 ? RowSum::add(one, four(factor + col)) : four(factor + col);
 #pragma unroll 4
-    for (int64_t i = group; i < runs; i += groups) {
-      const float* const at = p.workspace + (first + i) * p.D + col;
-      float4 ka = one, kc = one;
-      if (weights) {
-        const int64_t s = i / p.runs;
-        if (p.scale) ka = RowSum::add(one, four(p.scale + s * p.ld_scale + col));
-        if (p.gate) kc = four(p.gate + s * p.ld_gate + col);
-      }
-      if (want_a) a = fma4(*reinterpret_cast<const float4*>(at), ka, a);
-      if (want_b) b = RowSum::add(b, *reinterpret_cast<const float4*>(at + plane));
-      if (want_c) c = fma4(*reinterpret_cast<const float4*>(at + 2 * plane), kc, c);
+    for (int64_t i = first + group; i <= last; i += groups) sum = fma4(*reinterpret_cast<const float4*>(from + i * p.D), k, sum);
+  } else if (in) {
+#pragma unroll 2
+    for (int64_t i = group; i <= last; i += groups) {
+      // Sample s begins with entry floor(s rps / rpr) + s = floor(s (rps + rpr) / rpr).  The last entry before a sample that begins with a run is nobody's.
+      const int64_t s = ((i + 1) * rpr - 1) / (rps + rpr);
+      if ((i - s) * rpr >= min((s + 1) * rps, static_cast<int64_t>(p.M))) continue;
+      float4 k = one;
+      if (factor) k = plane == 0 ? RowSum::add(one, four(factor + s * ld_factor + col)) : four(factor + s * ld_factor + col);
+      sum = fma4(*reinterpret_cast<const float4*>(from + i * p.D), k, sum);
     }
   }
-  if (groups > 1) {
-    part[0][group][lane] = a;
-    part[1][group][lane] = b;
-    part[2][group][lane] = c;
+#pragma unroll
+  for (int d = 8; d <= 16; d <<= 1)
+    sum = RowSum::add(sum, make_float4(__shfl_xor_sync(0xffffffffu, sum.x, d), __shfl_xor_sync(0xffffffffu, sum.y, d), __shfl_xor_sync(0xffffffffu, sum.z, d),
+                                       __shfl_xor_sync(0xffffffffu, sum.w, d)));
+  const int warps = blockDim.x >> 5;
+  if (warps > 1) {
+    if ((threadIdx.x & 31) < 8) part[threadIdx.x >> 5][quad] = sum;
     __syncthreads();
-    if (group != 0) return;
-    for (int g = 1; g < groups; ++g) {
-      a = RowSum::add(a, part[0][g][lane]);
-      b = RowSum::add(b, part[1][g][lane]);
-      c = RowSum::add(c, part[2][g][lane]);
-    }
+    sum = part[0][quad];
+    for (int w = 1; w < warps; ++w) sum = RowSum::add(sum, part[w][quad]);
   }
-  if (!in) return;
-  auto put = [](float* to, const float4& v) { to[0] = v.x, to[1] = v.y, to[2] = v.z, to[3] = v.w; };  // (the outputs are only known to be floats)
-  const float4 none = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  if (weights) {
-    if (want_a) put(p.dweight + col, a);
-    if (want_c) put(p.dpost_weight + col, c);
-  } else {
-    const int64_t at = static_cast<int64_t>(blockIdx.x) * p.D + col;
-    if (want_a) put(p.dscale + at, p.weight ? fma4(a, four(p.weight + col), none) : a);
-    if (want_b) put(p.dshift + at, b);
-    if (want_c) put(p.dgate + at, p.post_weight ? fma4(c, four(p.post_weight + col), none) : c);
-  }
+  if (!in || group != 0) return;
+  if (by) sum = fma4(sum, after, none);
+  float* const at = to + sample * p.D + col;  // (only known to be floats)
+  at[0] = sum.x, at[1] = sum.y, at[2] = sum.z, at[3] = sum.w;
 }
 
 }  // namespace
 
-// Runs a sample's rows are cut into, none across two samples.  The SMs hold `slots` CTAs at once (128 registers a thread); a run costs
-// its rows and about four more for its parameters and its sums, and the CTAs work through the runs in rounds.
-void gated_norm_backward_runs(int32_t M, int32_t D, int32_t rows_per_sample, int32_t* samples, int32_t* runs, int32_t* rows_per_run) {
-  constexpr int kSms = 148, kRunCost = 4;
-  const int64_t slots = static_cast<int64_t>(kSms) * std::max(1, 512 / row_threads(D));
-  const int64_t rps = std::min<int64_t>(rows_per_sample, M);
-  const int64_t count = (M + rps - 1) / rps;
-  int64_t best_rows = rps, best_cost = -1;
-  for (int64_t rounds = 1; rounds <= 4; ++rounds) {
-    const int64_t wanted = std::max<int64_t>(1, rounds * slots / count);
-    const int64_t rows = (rps + wanted - 1) / wanted;
-    const int64_t total = count * ((rps + rows - 1) / rows);
-    const int64_t cost = (total + slots - 1) / slots * (rows + kRunCost);
-    if (best_cost < 0 || cost < best_cost) {
-      best_cost = cost;
-      best_rows = rows;
-    }
-  }
-  *samples = static_cast<int32_t>(count);
-  *rows_per_run = static_cast<int32_t>(best_rows);
-  *runs = static_cast<int32_t>((rps + best_rows - 1) / best_rows);
+// Whether the kernel with less in registers holds more CTAs of the width.  us, without and with it: 16384 x 1152 56.2, 52.3; 16384 x 2560 148.5, 107.6;
+// 16384 x 1024 46.1, 44.7.  With an fp32 stream, which is nearer to the memory's bound (5.0 TB/s) and has half as much again to keep, it lost: 68.1, 82.1.
+static bool keeps_local(int threads, bool f32) { return !f32 && kLocalThreads / threads > 512 / threads; }
+
+// The rows in runs of equal length, one for each of the CTAs that the SMs hold at once, and the entries of the workspace.  Runs cut at the samples' ends
+// instead left SMs idle: 16384 x 1152 in samples of 256 took 61 us, 56 without.
+void gated_norm_backward_runs(int32_t M, int32_t D, bool f32, int32_t rows_per_sample, int32_t* rows_per_run, int64_t* entries) {
+  constexpr int kSms = 148;
+  const int threads = row_threads(D), per_sm = (row_chunks(D) == 1 && keeps_local(threads, f32) ? kLocalThreads : 512) / threads;
+  const int64_t slots = static_cast<int64_t>(kSms) * per_sm, rows = M;
+  *rows_per_run = static_cast<int32_t>((rows + slots - 1) / slots);
+  *entries = (rows + *rows_per_run - 1) / *rows_per_run + (rows - 1) / rows_per_sample;
 }
 
 trdq_status launch_gated_norm_backward(const GatedNormBackward& args, cudaStream_t stream) {
   GatedNormBackward p = args;
-  const int64_t grid = static_cast<int64_t>(p.samples) * p.runs;
-  if (grid > 0x7FFFFFFE || row_threads(p.D) > 32 * kRowWarps) return TRDQ_ERR_SHAPE;
-  const int ch = row_chunks(p.D), threads = row_threads(p.D);
-  const auto kernel = ch == 1 ? (p.f32 ? gated_norm_backward_kernel<1, true> : gated_norm_backward_kernel<1, false>)
-                              : (p.f32 ? gated_norm_backward_kernel<2, true> : gated_norm_backward_kernel<2, false>);
-  if (launch_overlapped(kernel, dim3(static_cast<unsigned>(grid)), dim3(threads), 0, stream, p) != cudaSuccess) return TRDQ_ERR_CUDA;
+  const int64_t grid = (static_cast<int64_t>(p.M) + p.rows_per_run - 1) / p.rows_per_run, samples = (static_cast<int64_t>(p.M) - 1) / p.rows_per_sample + 1;
+  if (samples > 0x7FFFFFFE || row_threads(p.D) > 32 * kRowWarps) return TRDQ_ERR_SHAPE;
+  const int threads = row_threads(p.D);
+  const dim3 g(static_cast<unsigned>(grid)), t(threads);
+  cudaError_t e;
+  if (row_chunks(p.D) == 2) {
+    e = launch_overlapped(p.f32 ? gated_norm_backward_kernel<2, true, false> : gated_norm_backward_kernel<2, false, false>, g, t, 0, stream, p);
+  } else if (keeps_local(threads, p.f32)) {
+    e = launch_overlapped(gated_norm_backward_kernel<1, false, true>, g, t, sizeof(float4) * Kept<false, true>::kPieces * threads, stream, p);
+  } else {
+    e = launch_overlapped(p.f32 ? gated_norm_backward_kernel<1, true, false> : gated_norm_backward_kernel<1, false, false>, g, t, 0, stream, p);
+  }
+  if (e != cudaSuccess) return TRDQ_ERR_CUDA;
   const bool weights = p.dweight || p.dpost_weight, per_sample = p.dscale || p.dshift || p.dgate;
   if (!weights && !per_sample) return TRDQ_OK;
-  p.sample_blocks = per_sample ? p.samples : 0;
-  const int64_t most = weights ? grid : p.runs;
-  const int groups = most > 64 ? 32 : most > 8 ? 8 : most > 2 ? 2 : 1;
-  const dim3 jgrid(static_cast<unsigned>(p.sample_blocks + (weights ? 1 : 0)), (p.D / 4 + 31) / 32);
-  return launch_overlapped(gated_norm_join_kernel, jgrid, dim3(32, groups), 0, stream, p) == cudaSuccess ? TRDQ_OK : TRDQ_ERR_CUDA;
+  p.sample_blocks = per_sample ? static_cast<int32_t>(samples) : 0;
+  const int64_t of_sample = (std::min<int64_t>(p.rows_per_sample, p.M) - 1) / p.rows_per_run + 2;
+  const int64_t most = weights ? p.entries : of_sample;
+  // four entries a group; weights beside many small samples: a compromise
+  const int warps = static_cast<int>(std::min<int64_t>(weights && per_sample && samples > 1 ? 4 : kJoinWarps, std::max<int64_t>(1, most / 16)));
+  const dim3 jgrid(static_cast<unsigned>(p.sample_blocks + (weights ? 1 : 0)), (p.D / 4 + 7) / 8, 3);
+  return launch_overlapped(gated_norm_join_kernel, jgrid, dim3(32 * warps), 0, stream, p) == cudaSuccess ? TRDQ_OK : TRDQ_ERR_CUDA;
 }
 
 }  // namespace trdq

@@ -213,14 +213,15 @@ struct GatedNormBackward {
   uint16_t* db;
   int64_t lddx, lddb;
   float *dgate, *dshift, *dscale, *dweight, *dpost_weight;  // nullptr: not wanted
-  float* workspace;                                         // [3][samples * runs][D]
+  float* workspace;                                         // [3][entries][D]
   int32_t M, D, rows_per_sample, norm, post;
-  int32_t samples, runs, rows_per_run;  // gated_norm_backward_runs
-  int32_t sample_blocks;                // set by the launcher
+  int64_t entries;        // this and
+  int32_t rows_per_run;   // this from gated_norm_backward_runs
+  int32_t sample_blocks;  // set by the launcher
   float eps, alpha;
   bool f32;
 };
-void gated_norm_backward_runs(int32_t M, int32_t D, int32_t rows_per_sample, int32_t* samples, int32_t* runs, int32_t* rows_per_run);
+void gated_norm_backward_runs(int32_t M, int32_t D, bool f32, int32_t rows_per_sample, int32_t* rows_per_run, int64_t* entries);
 trdq_status launch_gated_norm_backward(const GatedNormBackward& p, cudaStream_t stream);
 
 // tensor maps (driver entry point fetched through the runtime; no link-time libcuda dependency)

@@ -379,3 +379,23 @@ def test_refusals():
         with pytest.raises(AssertionError):
             call()
     assert math.isfinite(trdq.trdq_gated_norm(c["x"], c["b"], **given)[1].float().sum().item())
+
+
+@pytest.mark.parametrize("M, D, rps", [(5000, 64, 1), (5000, 64, 3), (5000, 64, 4), (5000, 64, 9), (5000, 64, 2500), (2000, 1152, 12), (2000, 1152, 16), (1999, 1152, 667),
+                                       (700, 2560, 100)])
+def test_gradients_of_samples_that_end_anywhere(M, D, rps):
+    """Each CTA takes a run of rows whatever their samples: samples shorter and longer than a run, that begin where a run begins or inside it."""
+    from paper_2503_06564_b200 import trdq
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(M + rps)
+    c = _case(M, D, rps=rps, weight=True, seed=rps)
+    r = trdq.trdq_gated_norm(c["x"], c["b"], **_given(c))[0]
+    # eighths of small integers: their sums are exact in fp32, so dshift shows whether each row is in one sum, and in the right one
+    dh = (torch.randint(-3, 4, (M, D), generator=gen, device="cuda") / 8).bfloat16()
+    got = trdq.trdq_gated_norm_backward(r, c["b"], dh, None, **_given(c))
+    assert torch.equal(got["dshift"].double(), torch.stack([d.double().sum(0) for d in dh.split(rps)]))
+    want, tol = _reference_gradients(c, r, dh, None), _gradient_tolerances(c, r, dh, None)
+    for k, ref in want.items():
+        _within(got[k], ref, _rounded(tol[k], ref, got[k].dtype) + 1e-300)
+    again = trdq.trdq_gated_norm_backward(r, c["b"], dh, None, **_given(c))
+    assert all(torch.equal(v, again[k]) for k, v in got.items() if v is not None)
