@@ -33,37 +33,55 @@ __device__ __forceinline__ void load_chunks(const uint16_t* src, bool valid, uin
   for (int c = 0; c < 4; ++c) raw[c] = valid ? __ldg(reinterpret_cast<const uint4*>(src) + 4 * c) : make_uint4(0u, 0u, 0u, 0u);
 }
 
-// A warp takes one 128-block of eight consecutive rows: its lanes share the block's part of the fused vector, and its eight
-// scales are consecutive floats of scales[b][m].
+// A warp takes one 128-block of `steps` times eight consecutive rows: its lanes share the block's part of the fused vector, which stays in registers, and
+// the eight scales of a step are consecutive floats of scales[b][m].  The next step's values are requested before this one's are used.  Plain it is bound by
+// memory (5.8 TB/s at 32768 x 1152); rotated by instruction issue, 144 packed operations on 32 values beside 64 shuffles (24.9 us, 4.6 TB/s; read again
+// for each step the vector cost as much of the first-level cache as the values: 28.6 us).  Two CTAs an SM: with the registers of three it spills, 38 us.
 template <bool ROTATE>
-__global__ void __launch_bounds__(kThreads) fp8_quantize_kernel(const uint16_t* __restrict__ x, int64_t ldx, int32_t M, int32_t K,
+__global__ void __launch_bounds__(kThreads, 2) fp8_quantize_kernel(const uint16_t* __restrict__ x, int64_t ldx, int32_t M, int32_t K,
                                                                 const float* __restrict__ vec, uint8_t* __restrict__ codes,
-                                                                float* __restrict__ scales) {
+                                                                float* __restrict__ scales, int32_t steps) {
   const int nb = K / TRDQ_BLOCK;
   const int lane4 = threadIdx.x & (kFastLanes - 1);
   const int64_t item = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) >> 5;
   const int b = static_cast<int>(item % nb);
-  const int64_t row = item / nb * kRowsPerWarp + ((threadIdx.x & 31) / kFastLanes);
-  const bool valid = row < M;
+  int64_t row = item / nb * kRowsPerWarp * steps + ((threadIdx.x & 31) / kFastLanes);
   const int col0 = b * TRDQ_BLOCK + lane4 * 8;
   griddep_launch_dependents();
   griddep_wait();  // x may be written, and the codes still read, by the kernel before
   uint4 raw[4];
-  load_chunks(x + row * ldx + col0, valid, raw);
-  float2 v[16];
+  load_chunks(x + row * ldx + col0, row < M, raw);
+  float2 by[16];
   if constexpr (ROTATE) {
-    scale_chunks_lanes4(raw, reinterpret_cast<const float2*>(vec + col0), v);
-    wht128_lanes4(v, lane4);
-  } else {
-    widen_chunks_lanes4(raw, v);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float4 f = __ldg(reinterpret_cast<const float4*>(vec + col0 + 32 * c) + h);
+        by[4 * c + 2 * h] = make_float2(f.x, f.y);
+        by[4 * c + 2 * h + 1] = make_float2(f.z, f.w);
+      }
+    }
   }
-  const Fp8Factor f = fp8_factor(absmax_lanes4(v));
-  if (!valid) return;
-  fp8_store_lanes4(v, f.mul, codes + row * K + col0);
-  if (lane4 == 0) scales[static_cast<int64_t>(b) * M + row] = f.scale;
+  for (int i = 0; i < steps; ++i, row += kRowsPerWarp) {
+    float2 v[16];
+    widen_chunks_lanes4(raw, v);
+    if (i + 1 < steps) load_chunks(x + (row + kRowsPerWarp) * ldx + col0, row + kRowsPerWarp < M, raw);
+    if constexpr (ROTATE) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) v[j] = __fmul2_rn(v[j], by[j]);
+      wht128_lanes4(v, lane4);
+    }
+    const Fp8Factor f = fp8_factor(absmax_lanes4(v));
+    if (row < M) {
+      fp8_store_lanes4(v, f.mul, codes + row * K + col0);
+      if (lane4 == 0) scales[static_cast<int64_t>(b) * M + row] = f.scale;
+    }
+  }
 }
 
-// One CTA per 128 x 128 block of the weights, four threads a row.
+// One CTA per 128 x 128 block of the weights, four threads a row: the scale needs the whole block, which stays in registers meanwhile.  4608 x 1152: 7.0 us, the
+// launch, two latencies and the issue of the 324 blocks on 148 SMs.  (Registers for three CTAs an SM instead of two: spills, 7.3 us.)
 template <bool ROTATE>
 __global__ void __launch_bounds__(512) fp8_quantize_weights_kernel(const uint16_t* __restrict__ w, int32_t N, int32_t K, const float* __restrict__ vec,
                                                                    uint8_t* __restrict__ codes, float* __restrict__ scales) {
@@ -98,11 +116,16 @@ __global__ void __launch_bounds__(512) fp8_quantize_weights_kernel(const uint16_
 
 trdq_status launch_fp8_quantize(const void* x_bf16, int64_t ldx, int32_t M, int32_t K, const float* vec, uint8_t* codes, float* scales,
                                 cudaStream_t stream) {
-  const int64_t warps = (static_cast<int64_t>(M) + kRowsPerWarp - 1) / kRowsPerWarp * (K / TRDQ_BLOCK);
+  const int64_t groups = (static_cast<int64_t>(M) + kRowsPerWarp - 1) / kRowsPerWarp;
+  // More steps a warp while every SM still has its sixteen warps.  Eight against one: 32768 x 1152 rotated 24.9 us, 36.8; plain, where there is no vector
+  // to keep, four: 19.8 us, 21.8 for one and 23.0 for eight.
+  int32_t steps = 1;
+  while (steps < (vec ? 8 : 4) && groups * (K / TRDQ_BLOCK) / (2 * steps) >= 148 * 16) steps *= 2;
+  const int64_t warps = (groups + steps - 1) / steps * (K / TRDQ_BLOCK);
   const int64_t grid = (warps * 32 + kThreads - 1) / kThreads;
   if (grid > 0x7FFFFFFF) return TRDQ_ERR_SHAPE;
   const cudaError_t e = launch_overlapped(vec ? fp8_quantize_kernel<true> : fp8_quantize_kernel<false>, dim3(static_cast<unsigned>(grid)), dim3(kThreads), 0,
-                                          stream, static_cast<const uint16_t*>(x_bf16), ldx, M, K, vec, codes, scales);
+                                          stream, static_cast<const uint16_t*>(x_bf16), ldx, M, K, vec, codes, scales, steps);
   return e == cudaSuccess ? TRDQ_OK : TRDQ_ERR_CUDA;
 }
 

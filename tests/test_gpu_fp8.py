@@ -220,3 +220,18 @@ def test_refusals():
                  lambda: trdq.trdq_fp8_quantize(x.t().contiguous().t())):
         with pytest.raises(AssertionError):
             call()
+
+
+@pytest.mark.parametrize("M, K", [(9501, 4096), (4800, 4096), (20005, 1152)])
+@pytest.mark.parametrize("rotated", [False, True])
+def test_quantize_many_rows_as_few(M, K, rotated):
+    """A warp takes several steps of rows where there are many: the codes and scales are those of the same rows quantized a few at a time."""
+    import torch
+    from paper_2503_06564_b200 import trdq
+    gen = torch.Generator(device="cuda").manual_seed(M + K)
+    x = (torch.randn((M, K), generator=gen, device="cuda") * torch.exp(torch.randn((M, 1), generator=gen, device="cuda"))).bfloat16()
+    rot = _rotation(np.random.default_rng(1), K)[0] if rotated else None
+    codes, scales = trdq.trdq_fp8_quantize(x, rot, 200)
+    for at in range(0, M, 509):
+        few = trdq.trdq_fp8_quantize(x[at:at + 509], rot, 200)
+        assert torch.equal(codes[at:at + 509].view(torch.uint8), few[0].view(torch.uint8)) and torch.equal(scales[:, at:at + 509], few[1])
