@@ -258,11 +258,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
         const float4 ba = *reinterpret_cast<const float4*>(my_bias + 8 * v), bb = *reinterpret_cast<const float4*>(my_bias + 8 * v + 4);
         const float2 bias[4] = {make_float2(ba.x, ba.y), make_float2(ba.z, ba.w), make_float2(bb.x, bb.y), make_float2(bb.z, bb.w)};
         uint32_t packed[4];
+        float2 y[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float2 y = __fadd2_rn(acc[4 * v + j], bias[j]);
-          if constexpr (ACT) y = gelu_tanh2<false>(y);
-          packed[j] = pack_bf16(y);
+        for (int j = 0; j < 4; ++j) y[j] = __fadd2_rn(acc[4 * v + j], bias[j]);
+        if constexpr (ACT) {
+          gelu_pack<4>(y, packed);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) packed[j] = pack_bf16(y[j]);
         }
         st_shared_v4(my_stage + d.lane * 128 + ((v ^ (d.lane & 7)) << 4), packed[0], packed[1], packed[2], packed[3]);
       }
