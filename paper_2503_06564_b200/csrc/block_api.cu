@@ -227,7 +227,6 @@ trdq_status trdq_gated_norm_backward(const trdq_gated_norm_op* op, const void* d
   p.D = op->D;
   p.norm = op->norm;
   p.post = op->post_norm;
-  p.sample_blocks = 0;
   p.eps = op->eps;
   p.alpha = op->res_scale;
   p.f32 = op->stream_f32 != 0;

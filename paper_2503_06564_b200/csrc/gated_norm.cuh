@@ -68,6 +68,8 @@ __device__ __forceinline__ char* stream_at(void* base, int64_t row, int64_t ld, 
 // Chunk of a bf16 parameter row that may be absent.
 __device__ __forceinline__ uint4 load_param(const uint16_t* row, int chunk) { return __ldg(reinterpret_cast<const uint4*>(row) + chunk); }
 
+__device__ __forceinline__ void prefetch_l1(const void* at) { asm volatile("prefetch.global.L1 [%0];" ::"l"(at)); }
+
 __device__ __forceinline__ float chunk_sum(const Chunk& c) {
   const float2 s = __fadd2_rn(__fadd2_rn(c.p[0], c.p[1]), __fadd2_rn(c.p[2], c.p[3]));
   return __fadd_rn(s.x, s.y);

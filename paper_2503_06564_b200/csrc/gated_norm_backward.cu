@@ -180,6 +180,12 @@ __global__ void __launch_bounds__(LOCAL ? kLocalThreads : 32 * kRowWarps, 1) gat
       A[j] = B[j] = C[j] = none;
     }
   };
+  auto prefetch = [&](const uint16_t* param, int64_t ld) {
+    if (!param) return;
+#pragma unroll
+    for (int j = 0; j < CH; ++j)
+      if (in[j]) prefetch_l1(param + (s + 1) * ld + 8 * at[j]);
+  };
   begin();
   const float2 alpha2 = make_float2(p.alpha, p.alpha);
   for (int row = 0; row < rows; ++row) {
@@ -188,6 +194,10 @@ __global__ void __launch_bounds__(LOCAL ? kLocalThreads : 32 * kRowWarps, 1) gat
       ++s;
       until = static_cast<int>(min(static_cast<int64_t>(until) + p.rows_per_sample, static_cast<int64_t>(rows)));
       begin();
+    }
+    if (row + 2 == until && until < rows) {  // soon the next sample's parameters
+      prefetch(p.scale, p.ld_scale);
+      prefetch(p.gate, p.ld_gate);
     }
     Chunk n[CH], m[CH], dh[CH], dR[CH];
 #pragma unroll
@@ -264,38 +274,74 @@ __global__ void __launch_bounds__(LOCAL ? kLocalThreads : 32 * kRowWarps, 1) gat
   flush();
 }
 
-// Joins the entries of one of the three planes (blockIdx.z), 32 columns a CTA, four a thread.  blockIdx.x < sample_blocks: a sample's gradients, from the
-// entries of the runs that it has rows of; the CTAs behind them: the weights' gradients, from all entries.  The groups of eight threads take every
-// `groups`-th entry; their sums are added in order.  Bound by latency: with 128 columns and all three planes in one CTA the sums of 130 runs of 4096 took 7 us instead of 5.
+__device__ __forceinline__ float4 widen4(const uint16_t* v) {
+  const uint2 w = *reinterpret_cast<const uint2*>(v);
+  const float2 a = widen_bf16x2(w.x), b = widen_bf16x2(w.y);
+  return make_float4(a.x, a.y, b.x, b.y);
+}
+__device__ __forceinline__ float4 fma4(const float4& a, const float4& b, const float4& c) {
+  return make_float4(__fmaf_rn(a.x, b.x, c.x), __fmaf_rn(a.y, b.y, c.y), __fmaf_rn(a.z, b.z, c.z), __fmaf_rn(a.w, b.w, c.w));
+}
+// (the outputs are only known to be floats)
+__device__ __forceinline__ void put4(float* to, const float4& v) { to[0] = v.x, to[1] = v.y, to[2] = v.z, to[3] = v.w; }
+__device__ __forceinline__ float4 ones4() { return make_float4(1.0f, 1.0f, 1.0f, 1.0f); }
+__device__ __forceinline__ float4 zeros4() { return make_float4(0.0f, 0.0f, 0.0f, 0.0f); }
+
+// What a plane's sums become: a sample's gradient, and the parameter that multiplies it.
+__device__ __forceinline__ float* sample_output(const GatedNormBackward& p, int plane) { return plane == 0 ? p.dscale : plane == 1 ? p.dshift : p.dgate; }
+__device__ __forceinline__ const uint16_t* sample_factor(const GatedNormBackward& p, int plane) { return plane == 0 ? p.weight : plane == 1 ? nullptr : p.post_weight; }
+
+// The first and last entry of a sample, one for each run that it has rows of.
+__device__ __forceinline__ void sample_entries(const GatedNormBackward& p, int64_t sample, int64_t* first, int64_t* last) {
+  const int64_t end = min((sample + 1) * p.rows_per_sample, static_cast<int64_t>(p.M));
+  *first = sample * p.rows_per_sample / p.rows_per_run + sample;
+  *last = (end - 1) / p.rows_per_run + sample;
+}
+
+// Joins samples of few entries: a thread takes four columns of a plane of a sample and adds its entries in order.  The whole call with this join and with the
+// one below, us: 16384 x 1152 in samples of 256 rows, ten entries each, 50, 52; 18846 x 680 in samples of 16 45, 79; 4096 x 1152 in samples of one 60, 258.
+__global__ void __launch_bounds__(256) gated_norm_join_samples_kernel(const GatedNormBackward p) {
+  const int quads = p.D / 4;
+  const int64_t item = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, of = item / quads;
+  const int col = static_cast<int>(item - of * quads) * 4, plane = blockIdx.y;
+  float* const to = sample_output(p, plane);
+  if (!to || of > (p.M - 1) / p.rows_per_sample) return;
+  int64_t first, last;
+  sample_entries(p, of, &first, &last);
+  const float* const from = p.workspace + plane * p.entries * p.D + col;
+  const uint16_t* const by = sample_factor(p, plane);
+  griddep_wait();
+  const float4 after = by ? widen4(by + col) : ones4();
+  float4 sum = zeros4();
+#pragma unroll 4
+  for (int64_t i = first; i <= last; ++i) sum = RowSum::add(sum, *reinterpret_cast<const float4*>(from + i * p.D));
+  put4(to + of * p.D + col, by ? fma4(sum, after, zeros4()) : sum);
+}
+
+// Joins many entries of one of the planes (blockIdx.z), 32 columns a CTA, four a thread.  WEIGHTS: the weights' gradients, from all entries; else those of the
+// sample blockIdx.x.  The groups of eight threads take every `groups`-th entry; their sums are added in order.  Bound by latency: with 128 columns
+// and all three planes in one CTA the sums of 130 runs of 4096 took 7 us instead of 5.
+template <bool WEIGHTS>
 __global__ void __launch_bounds__(32 * kJoinWarps) gated_norm_join_kernel(const GatedNormBackward p) {
   __shared__ float4 part[kJoinWarps][8];
   const int quad = threadIdx.x & 7, group = threadIdx.x >> 3, groups = blockDim.x >> 3, plane = blockIdx.z;
   const int col = (blockIdx.y * 8 + quad) * 4;
-  const bool in = col < p.D, weights = blockIdx.x >= static_cast<unsigned>(p.sample_blocks);
-  float* const to = plane == 0 ? (weights ? p.dweight : p.dscale) : plane == 1 ? (weights ? nullptr : p.dshift) : weights ? p.dpost_weight : p.dgate;
+  const bool in = col < p.D;
+  float* const to = !WEIGHTS ? sample_output(p, plane) : plane == 0 ? p.dweight : plane == 1 ? nullptr : p.dpost_weight;
   if (!to) return;
   const int64_t rps = p.rows_per_sample, rpr = p.rows_per_run;
-  const int64_t sample = weights ? 0 : blockIdx.x, end = min((sample + 1) * rps, static_cast<int64_t>(p.M));
-  const int64_t first = sample * rps / rpr + sample, last = weights ? p.entries - 1 : (end - 1) / rpr + sample;
-  const uint16_t* const factor = !weights ? nullptr : plane == 0 ? p.scale : p.gate;
+  int64_t first = 0, last = p.entries - 1;
+  if (!WEIGHTS) sample_entries(p, blockIdx.x, &first, &last);
+  const uint16_t* const factor = !WEIGHTS ? nullptr : plane == 0 ? p.scale : p.gate;
   const int64_t ld_factor = plane == 0 ? p.ld_scale : p.ld_gate;
   const float* const from = p.workspace + plane * p.entries * p.D + col;
+  const uint16_t* const by = WEIGHTS ? nullptr : sample_factor(p, plane);
   griddep_wait();
-  auto four = [](const uint16_t* v) {
-    const uint2 w = *reinterpret_cast<const uint2*>(v);
-    const float2 a = widen_bf16x2(w.x), b = widen_bf16x2(w.y);
-    return make_float4(a.x, a.y, b.x, b.y);
-  };
-  const float4 none = make_float4(0.0f, 0.0f, 0.0f, 0.0f), one = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
-  auto fma4 = [](const float4& a, const float4& b, const float4& c) {
-    return make_float4(__fmaf_rn(a.x, b.x, c.x), __fmaf_rn(a.y, b.y, c.y), __fmaf_rn(a.z, b.z, c.z), __fmaf_rn(a.w, b.w, c.w));
-  };
-  const uint16_t* const by = weights ? nullptr : plane == 0 ? p.weight : plane == 2 ? p.post_weight : nullptr;
-  const float4 after = by && in ? four(by + col) : one;
-  float4 sum = none;
-  if (in && (!weights || rps >= p.M)) {
-    float4 k = one;
-    if (factor) k = plane == 0 ? RowSum::add(one, four(factor + col)) : four(factor + col);
+  const float4 after = by && in ? widen4(by + col) : ones4();
+  float4 sum = zeros4();
+  if (in && (!WEIGHTS || rps >= p.M)) {
+    float4 k = ones4();
+    if (factor) k = plane == 0 ? RowSum::add(k, widen4(factor + col)) : widen4(factor + col);
 #pragma unroll 4
     for (int64_t i = first + group; i <= last; i += groups) sum = fma4(*reinterpret_cast<const float4*>(from + i * p.D), k, sum);
   } else if (in) {
@@ -304,8 +350,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps) gated_norm_join_kernel(const 
       // Sample s begins with entry floor(s rps / rpr) + s = floor(s (rps + rpr) / rpr).  The last entry before a sample that begins with a run is nobody's.
       const int64_t s = ((i + 1) * rpr - 1) / (rps + rpr);
       if ((i - s) * rpr >= min((s + 1) * rps, static_cast<int64_t>(p.M))) continue;
-      float4 k = one;
-      if (factor) k = plane == 0 ? RowSum::add(one, four(factor + s * ld_factor + col)) : four(factor + s * ld_factor + col);
+      float4 k = ones4();
+      if (factor) k = plane == 0 ? RowSum::add(k, widen4(factor + s * ld_factor + col)) : widen4(factor + s * ld_factor + col);
       sum = fma4(*reinterpret_cast<const float4*>(from + i * p.D), k, sum);
     }
   }
@@ -321,9 +367,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) gated_norm_join_kernel(const 
     for (int w = 1; w < warps; ++w) sum = RowSum::add(sum, part[w][quad]);
   }
   if (!in || group != 0) return;
-  if (by) sum = fma4(sum, after, none);
-  float* const at = to + sample * p.D + col;  // (only known to be floats)
-  at[0] = sum.x, at[1] = sum.y, at[2] = sum.z, at[3] = sum.w;
+  put4(to + (WEIGHTS ? 0 : static_cast<int64_t>(blockIdx.x) * p.D) + col, by ? fma4(sum, after, zeros4()) : sum);
 }
 
 }  // namespace
@@ -357,15 +401,22 @@ trdq_status launch_gated_norm_backward(const GatedNormBackward& args, cudaStream
     e = launch_overlapped(p.f32 ? gated_norm_backward_kernel<1, true, false> : gated_norm_backward_kernel<1, false, false>, g, t, 0, stream, p);
   }
   if (e != cudaSuccess) return TRDQ_ERR_CUDA;
-  const bool weights = p.dweight || p.dpost_weight, per_sample = p.dscale || p.dshift || p.dgate;
-  if (!weights && !per_sample) return TRDQ_OK;
-  p.sample_blocks = per_sample ? static_cast<int32_t>(samples) : 0;
-  const int64_t of_sample = (std::min<int64_t>(p.rows_per_sample, p.M) - 1) / p.rows_per_run + 2;
-  const int64_t most = weights ? p.entries : of_sample;
-  // four entries a group; weights beside many small samples: a compromise
-  const int warps = static_cast<int>(std::min<int64_t>(weights && per_sample && samples > 1 ? 4 : kJoinWarps, std::max<int64_t>(1, most / 16)));
-  const dim3 jgrid(static_cast<unsigned>(p.sample_blocks + (weights ? 1 : 0)), (p.D / 4 + 7) / 8, 3);
-  return launch_overlapped(gated_norm_join_kernel, jgrid, dim3(32 * warps), 0, stream, p) == cudaSuccess ? TRDQ_OK : TRDQ_ERR_CUDA;
+  auto warps_for = [](int64_t entries) { return static_cast<unsigned>(std::min<int64_t>(kJoinWarps, std::max<int64_t>(1, entries / 16))); };  // four a group
+  const unsigned blocks32 = (p.D / 4 + 7) / 8;
+  if (p.dscale || p.dshift || p.dgate) {
+    const int64_t most = (std::min<int64_t>(p.rows_per_sample, p.M) - 1) / p.rows_per_run + 2;  // entries of a sample
+    if (most <= 16) {
+      const int64_t ctas = (samples * (p.D / 4) + 255) / 256;
+      if (ctas > 0x7FFFFFFF) return TRDQ_ERR_SHAPE;
+      e = launch_overlapped(gated_norm_join_samples_kernel, dim3(static_cast<unsigned>(ctas), 3), dim3(256), 0, stream, p);
+    } else {
+      e = launch_overlapped(gated_norm_join_kernel<false>, dim3(static_cast<unsigned>(samples), blocks32, 3), dim3(32 * warps_for(most)), 0, stream, p);
+    }
+    if (e != cudaSuccess) return TRDQ_ERR_CUDA;
+  }
+  if (p.dweight || p.dpost_weight)
+    e = launch_overlapped(gated_norm_join_kernel<true>, dim3(1, blocks32, 3), dim3(32 * warps_for(p.entries)), 0, stream, p);
+  return e == cudaSuccess ? TRDQ_OK : TRDQ_ERR_CUDA;
 }
 
 }  // namespace trdq

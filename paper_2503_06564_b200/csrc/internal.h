@@ -217,7 +217,6 @@ struct GatedNormBackward {
   int32_t M, D, rows_per_sample, norm, post;
   int64_t entries;        // this and
   int32_t rows_per_run;   // this from gated_norm_backward_runs
-  int32_t sample_blocks;  // set by the launcher
   float eps, alpha;
   bool f32;
 };
