@@ -56,7 +56,7 @@ def _calls_command(out: str) -> list:
                sysconfig.get_paths()["include"], os.path.join(toolkit, "include")]
     return [os.environ.get("CXX", "g++"), "-std=c++17", "-O2", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
             *(f"-I{d}" for d in include), os.path.join(CSRC, "calls.cpp"), "-o", out,
-            "-L" + os.path.join(base, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+            "-L" + os.path.join(base, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda"]
 
 
 def _stale() -> bool:

@@ -11,6 +11,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
@@ -125,7 +126,7 @@ class Outputs {
       void* pointers[kMost];
       for (int i = 0; i < n_; ++i) {
         Item& o = item_[i];
-        if (!o.given) o.made = at::empty(at::IntArrayRef(o.sizes, o.dims), options_.dtype(o.type));
+        if (!o.given) o.made = at::detail::empty_cuda(at::IntArrayRef(o.sizes, o.dims), o.type, options_.device(), c10::nullopt);
         pointers[i] = o.given ? o.pointer : o.made.data_ptr();
       }
       st = call(pointers);
