@@ -11,7 +11,9 @@
 // running sums stay in its registers.  The runs are of equal length, one for each CTA that the SMs hold, and cross the samples: where a sample ends, and at the
 // end of the run, the sums go to the workspace, run c's of sample s to entry c + s (each step along the rows moves to the next run, the
 // next sample or both, so no entry is used twice).  A second kernel joins them in a fixed order: equal inputs give equal gradients.  The statistics are taken again from r and b, which are in registers for the gradient itself.
-// What bounds it: memory, 12 bytes a channel with a bf16 stream.
+// What bounds it: the latencies of three row sums a row with as many rows in flight as registers allow, beside memory, 12 bytes a channel with a bf16 stream.
+// 16384 x 1152 (adaLN) 50 us, 4.5 TB/s of a measured 6.6, 44 without the parameters' gradients; 517 x 4096 (fp32 stream, both norms) 17.5 us.
+// Measured and not better: the row sums in two rounds in place of three or four (registers spill: 63 us).
 #include <algorithm>
 
 #include "gated_norm.cuh"
