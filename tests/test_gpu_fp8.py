@@ -235,3 +235,33 @@ def test_quantize_many_rows_as_few(M, K, rotated):
     for at in range(0, M, 509):
         few = trdq.trdq_fp8_quantize(x[at:at + 509], rot, 200)
         assert torch.equal(codes[at:at + 509].view(torch.uint8), few[0].view(torch.uint8)) and torch.equal(scales[:, at:at + 509], few[1])
+
+
+@pytest.mark.parametrize("M, N, K", [(32, 16384, 128), (64, 16384, 256), (96, 16384, 512), (200, 16384, 128), (256, 1152, 4608), (9, 4608, 4608), (16, 160, 16384), (130, 1040, 2176),
+                                     (600, 4096, 256)])
+@pytest.mark.parametrize("act", [0, 1])
+def test_linear_cuts(M, N, K, act):
+    """One and two CTAs an SM, more tiles than fit, tiles whose channel blocks are shared by two to eight CTAs, blocks that do not divide evenly, and the first sizes of the pairs."""
+    _check_linear(M, N, K, act, seed=M + N + K)
+    _check_linear(M, N, K, act, pad=8, bias=False, seed=M * 3 + N + K)
+
+
+def test_linear_of_a_bad_channel_and_a_bad_row():
+    """A NaN in a weight's channel spoils that column and no other, one among a row's codes that row, with the activation too."""
+    import torch
+    from paper_2503_06564_b200 import trdq
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    for M in (3, 40, 700):
+        K, N = 1152, 1040
+        x, w = torch.randn((M, K), generator=gen, device="cuda").bfloat16(), torch.randn((N, K), generator=gen, device="cuda").bfloat16()
+        (q, sx), (qw, sw) = trdq.trdq_fp8_quantize(x), trdq.trdq_fp8_quantize_weights(w)
+        for act in (0, 1):
+            want = trdq.trdq_fp8_linear(q, sx, qw, sw, act=act)
+            bad_q, bad_w = q.clone().view(torch.uint8), qw.clone().view(torch.uint8)
+            bad_q[M // 2, 700] = 0x7F
+            bad_w[517, 3] = 0xFF
+            y = trdq.trdq_fp8_linear(bad_q.view(q.dtype), sx, bad_w.view(q.dtype), sw, act=act)
+            spoilt = torch.zeros((M, N), dtype=torch.bool, device="cuda")
+            spoilt[M // 2] = True
+            spoilt[:, 517] = True
+            assert torch.equal(y.isnan(), spoilt) and torch.equal(y[~spoilt], want[~spoilt])
