@@ -33,6 +33,7 @@ struct StreamChunk<false> {
   uint4 w;
   __device__ __forceinline__ void clear() { w = zero4(); }
   __device__ __forceinline__ void load(const void* at) { w = *static_cast<const uint4*>(at); }
+  __device__ __forceinline__ void load_pieces(const float4* at, int) { load(at); }  // 16-byte pieces, `step` of them from one to the next
   __device__ __forceinline__ void store(void* at) const { *static_cast<uint4*>(at) = w; }
   __device__ __forceinline__ Chunk value() const { return widen(w); }
   __device__ __forceinline__ void set(const Chunk& c) { w = narrow(c); }  // rounds
@@ -44,6 +45,10 @@ struct StreamChunk<true> {
   __device__ __forceinline__ void load(const void* at) {
     lo = static_cast<const float4*>(at)[0];
     hi = static_cast<const float4*>(at)[1];
+  }
+  __device__ __forceinline__ void load_pieces(const float4* at, int step) {
+    lo = at[0];
+    hi = at[step];
   }
   __device__ __forceinline__ void store(void* at) const {
     static_cast<float4*>(at)[0] = lo;

@@ -34,8 +34,8 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) { asm 
 __device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 // What a thread keeps between rows besides its sums: its columns' two parameters, and the inputs of the next row, which are on their way while this row is
-// computed.  In registers (LOCAL false), or in 16-byte pieces of shared memory that no other thread touches, `step` threads apart (LOCAL true): 96 registers
-// instead of 128, so five warps a scheduler and not four.
+// computed.  In registers (LOCAL false), or in 16-byte pieces of shared memory that no other thread touches, `step` threads apart (LOCAL true): with one chunk a
+// thread 96 registers instead of 128, so five warps a scheduler and not four; with two, what else would spill.
 template <bool F32, bool LOCAL>
 struct Kept;
 template <bool F32>
@@ -58,16 +58,17 @@ struct Kept<F32, false> {
   }
   __device__ __forceinline__ RowInputs<F32> get() const { return next; }
 };
-template <>
-struct Kept<false, true> {
-  static constexpr int kPieces = 8;  // r, dr, b, dh, two of each parameter
+template <bool F32>
+struct Kept<F32, true> {
+  static constexpr int kHalves = F32 ? 2 : 1;            // pieces of a chunk of the stream
+  static constexpr int kGain = 2 * kHalves + 2, kGate = kGain + 2, kPieces = kGate + 2;  // behind r, dr, b, dh
   float4* mine;
   int step;
   __device__ __forceinline__ void clear(float4* at, int threads) {
     mine = at;
     step = threads;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) mine[k * step] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int k = 0; k < kGain; ++k) mine[k * step] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   }
   __device__ __forceinline__ void put(int piece, const Chunk& c) {
     mine[piece * step] = make_float4(c.p[0].x, c.p[0].y, c.p[1].x, c.p[1].y);
@@ -78,35 +79,38 @@ struct Kept<false, true> {
     return Chunk{{make_float2(a.x, a.y), make_float2(a.z, a.w), make_float2(b.x, b.y), make_float2(b.z, b.w)}};
   }
   __device__ __forceinline__ void set_params(const Chunk& a, const Chunk& b) {
-    put(4, a);
-    put(6, b);
+    put(kGain, a);
+    put(kGate, b);
   }
-  __device__ __forceinline__ Chunk get_gain() const { return chunk(4); }
-  __device__ __forceinline__ Chunk get_gate() const { return chunk(6); }
+  __device__ __forceinline__ Chunk get_gain() const { return chunk(kGain); }
+  __device__ __forceinline__ Chunk get_gate() const { return chunk(kGate); }
   // (the pieces of the row before are in registers by now)
   __device__ __forceinline__ void request(const char* r, const char* dr, const char* b, const char* dh) {
     const uint32_t at = smem_u32(mine), by = static_cast<uint32_t>(step) * 16;
-    cp_async16(at, r);
-    if (dr) cp_async16(at + by, dr);
-    if (b) cp_async16(at + 2 * by, b);
-    cp_async16(at + 3 * by, dh);
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) {
+      cp_async16(at + h * by, r + 16 * h);
+      if (dr) cp_async16(at + (kHalves + h) * by, dr + 16 * h);
+    }
+    if (b) cp_async16(at + 2 * kHalves * by, b);
+    cp_async16(at + (2 * kHalves + 1) * by, dh);
   }
-  __device__ __forceinline__ RowInputs<false> get() const {
-    cp_async_wait_all();
-    RowInputs<false> v;
-    v.r.load(mine);
-    v.dr.load(mine + step);
-    v.b = *reinterpret_cast<const uint4*>(mine + 2 * step);
-    v.dh = *reinterpret_cast<const uint4*>(mine + 3 * step);
+  __device__ __forceinline__ RowInputs<F32> get() const {
+    RowInputs<F32> v;
+    v.r.load_pieces(mine, step);
+    v.dr.load_pieces(mine + kHalves * step, step);
+    v.b = *reinterpret_cast<const uint4*>(mine + 2 * kHalves * step);
+    v.dh = *reinterpret_cast<const uint4*>(mine + (2 * kHalves + 1) * step);
     return v;
   }
 };
 
-constexpr int kLocalThreads = 640;  // of an SM, with LOCAL
+constexpr int kLocalThreads = 640;  // of an SM, with LOCAL and one chunk a thread
+template <bool F32>
+constexpr int kLocalPieces = Kept<F32, true>::kPieces;
 
 template <int CH, bool F32, bool LOCAL>
-__global__ void __launch_bounds__(LOCAL ? kLocalThreads : 32 * kRowWarps, 1) gated_norm_backward_kernel(const GatedNormBackward p) {
-  static_assert(CH == 1 || !LOCAL, "one chunk's room a thread");
+__global__ void __launch_bounds__(LOCAL && CH == 1 ? kLocalThreads : 32 * kRowWarps, 1) gated_norm_backward_kernel(const GatedNormBackward p) {
   extern __shared__ float4 local[];
   __shared__ float4 slots[RowSum::kSlots];
   RowSum sums(slots);
@@ -138,7 +142,7 @@ __global__ void __launch_bounds__(LOCAL ? kLocalThreads : 32 * kRowWarps, 1) gat
 
   Kept<F32, LOCAL> kept[CH];
 #pragma unroll
-  for (int j = 0; j < CH; ++j) kept[j].clear(local + threadIdx.x, blockDim.x);  // what is not loaded (lanes outside the row, inputs that are not there) stays zero
+  for (int j = 0; j < CH; ++j) kept[j].clear(local + j * kLocalPieces<F32> * blockDim.x + threadIdx.x, blockDim.x);  // what is not loaded (lanes outside the row, inputs that are not there) stays zero
   auto fetch = [&](bool valid) {
 #pragma unroll
     for (int j = 0; j < CH; ++j) {
@@ -204,6 +208,7 @@ __global__ void __launch_bounds__(LOCAL ? kLocalThreads : 32 * kRowWarps, 1) gat
     Chunk n[CH], m[CH], dh[CH], dR[CH];
 #pragma unroll
     for (int j = 0; j < CH; ++j) {
+      if (LOCAL && j == 0) cp_async_wait_all();
       const RowInputs<F32> now = kept[j].get();
       n[j] = now.r.value();
       m[j] = widen(now.b);
@@ -396,9 +401,13 @@ trdq_status launch_gated_norm_backward(const GatedNormBackward& args, cudaStream
   const dim3 g(static_cast<unsigned>(grid)), t(threads);
   cudaError_t e;
   if (row_chunks(p.D) == 2) {
-    e = launch_overlapped(p.f32 ? gated_norm_backward_kernel<2, true, false> : gated_norm_backward_kernel<2, false, false>, g, t, 0, stream, p);
+    const auto kernel = p.f32 ? gated_norm_backward_kernel<2, true, true> : gated_norm_backward_kernel<2, false, true>;
+    const size_t bytes = sizeof(float4) * 2 * (p.f32 ? kLocalPieces<true> : kLocalPieces<false>) * threads;
+    // (on each call: the attribute belongs to the device)
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)) != cudaSuccess) return TRDQ_ERR_CUDA;
+    e = launch_overlapped(kernel, g, t, bytes, stream, p);
   } else if (keeps_local(threads, p.f32)) {
-    e = launch_overlapped(gated_norm_backward_kernel<1, false, true>, g, t, sizeof(float4) * Kept<false, true>::kPieces * threads, stream, p);
+    e = launch_overlapped(gated_norm_backward_kernel<1, false, true>, g, t, sizeof(float4) * kLocalPieces<false> * threads, stream, p);
   } else {
     e = launch_overlapped(p.f32 ? gated_norm_backward_kernel<1, true, false> : gated_norm_backward_kernel<1, false, false>, g, t, 0, stream, p);
   }
