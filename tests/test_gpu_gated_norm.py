@@ -399,3 +399,46 @@ def test_gradients_of_samples_that_end_anywhere(M, D, rps):
         _within(got[k], ref, _rounded(tol[k], ref, got[k].dtype) + 1e-300)
     again = trdq.trdq_gated_norm_backward(r, c["b"], dh, None, **_given(c))
     assert all(torch.equal(v, again[k]) for k, v in got.items() if v is not None)
+
+
+@pytest.mark.parametrize("M, D, rps", [(400, 4104, 7), (333, 8192, 100), (500, 5120, 500)])
+@pytest.mark.parametrize("stream", ["bf16", "fp32"])
+@pytest.mark.parametrize("post", ["none", "layer"])
+def test_gradients_of_wide_rows(M, D, rps, stream, post):
+    """Two chunks a thread, several rows and samples a run."""
+    from paper_2503_06564_b200 import trdq
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(M + D)
+    c = _case(M, D, rps=rps, stream=stream, post=post, weight=True, seed=D, alpha=0.5)
+    r = trdq.trdq_gated_norm(c["x"], c["b"], **_given(c))[0]
+    dh, dr = torch.randn((M, D), generator=gen, device="cuda").bfloat16(), torch.randn((M, D + 16), generator=gen, device="cuda").to(r.dtype)[:, :D]
+    got = trdq.trdq_gated_norm_backward(r, c["b"], dh, dr, **_given(c))
+    want, tol = _reference_gradients(c, r, dh, dr), _gradient_tolerances(c, r, dh, dr)
+    for k, ref in want.items():
+        _within(got[k], ref, _rounded(tol[k], ref, got[k].dtype) + 1e-300)
+    again = trdq.trdq_gated_norm_backward(r, c["b"], dh, dr, **_given(c))
+    assert all(torch.equal(v, again[k]) for k, v in got.items() if v is not None)
+
+
+@pytest.mark.parametrize("M, D, rps", [(3000, 1152, 1), (3001, 1152, 13), (2999, 640, 700), (900, 5120, 11)])
+@pytest.mark.parametrize("rotated", [False, True])
+def test_many_rows_as_few(M, D, rps, rotated):
+    """Runs of several rows a CTA, samples that change inside them: the bits of the same rows a sample at a time."""
+    from paper_2503_06564_b200 import trdq
+    import torch
+    c = _case(M, D, rps=rps, post="rms", weight=True, seed=M + D)
+    given = _given(c)
+    rot = None
+    if rotated:
+        rng = np.random.default_rng(3)
+        rot = trdq.Rotation(D, [0, 1000], (rng.integers(0, 2, (1, D)) * 2 - 1).astype(np.int8), rng.uniform(0.5, 2.0, (1, D)).astype(np.float32))
+    whole = trdq.trdq_gated_norm(c["x"], c["b"], **given) + trdq.trdq_gated_norm_fp8(rot, 5, c["x"], c["b"], **given)
+    for s in sorted({0, 1, (M // rps) // 2, (M - 1) // rps}):
+        rows, one = slice(s * rps, min(M, s * rps + rps)), dict(given)
+        one["rows_per_sample"] = rps
+        for name in ("gate", "shift", "scale"):
+            one[name] = given[name][s:s + 1]
+        part = trdq.trdq_gated_norm(c["x"][rows], c["b"][rows], **one) + trdq.trdq_gated_norm_fp8(rot, 5, c["x"][rows], c["b"][rows], **one)
+        for w, p in zip(whole, part):
+            w = w[rows] if w.shape[0] == M else w[:, rows]
+            assert torch.equal(w.contiguous().view(torch.uint8), p.contiguous().view(torch.uint8))
