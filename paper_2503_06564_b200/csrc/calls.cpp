@@ -104,6 +104,9 @@ bool output(PyObject* o, int32_t M, int64_t N, int64_t* ld) {
 
 void* stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
 
+// A new CUDA tensor from the allocator's own entry: what torch.empty gives, without the dispatch (no_modes() has been asked).
+at::Tensor new_tensor(at::IntArrayRef sizes, at::ScalarType type, at::Device device) { return at::detail::empty_cuda(sizes, type, device, c10::nullopt); }
+
 struct WithoutGil {
   PyThreadState* const state = PyEval_SaveThread();
   ~WithoutGil() { PyEval_RestoreThread(state); }
@@ -126,7 +129,7 @@ class Outputs {
       void* pointers[kMost];
       for (int i = 0; i < n_; ++i) {
         Item& o = item_[i];
-        if (!o.given) o.made = at::detail::empty_cuda(at::IntArrayRef(o.sizes, o.dims), o.type, options_.device(), c10::nullopt);
+        if (!o.given) o.made = new_tensor(at::IntArrayRef(o.sizes, o.dims), o.type, options_.device());
         pointers[i] = o.given ? o.pointer : o.made.data_ptr();
       }
       st = call(pointers);
@@ -537,7 +540,7 @@ PyObject* gated_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   for (int i = 1; i < 7; ++i) wanted[i] = a[i] != Py_None;
   GENERAL_WAY_UNLESS(block_entry.gated_norm_backward_workspace(&op, &bytes) == TRDQ_OK);
   void *const dh = pointer(a[12]), *const dr = pointer(a[13]);
-  const at::TensorOptions options = tensor(a[0]).options();
+  const at::Device where = tensor(a[0]).device();
   void* const s = stream();
   at::Tensor made[7];
   trdq_status st;
@@ -545,12 +548,12 @@ PyObject* gated_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     WithoutGil released;
     at::Tensor workspace;
     const bool sums = wanted[2] || wanted[3] || wanted[4] || wanted[5] || wanted[6];
-    if (sums) workspace = at::empty({static_cast<int64_t>(bytes > 16 ? bytes : 16)}, options.dtype(at::kByte));
+    if (sums) workspace = new_tensor({static_cast<int64_t>(bytes > 16 ? bytes : 16)}, at::kByte, where);
     for (int i = 0; i < 7; ++i) {
       if (!wanted[i]) continue;
       const int64_t rows = i < 2 ? op.M : samples;
-      const at::TensorOptions o = options.dtype(i == 0 ? type : i == 1 ? at::kBFloat16 : at::kFloat);
-      made[i] = i < 5 ? at::empty({rows, op.D}, o) : at::empty({op.D}, o);
+      const at::ScalarType o = i == 0 ? type : i == 1 ? at::kBFloat16 : at::kFloat;
+      made[i] = i < 5 ? new_tensor({rows, op.D}, o, where) : new_tensor({op.D}, o, where);
     }
     auto at_ = [&](int i) { return wanted[i] ? static_cast<float*>(made[i].data_ptr()) : nullptr; };
     st = block_entry.gated_norm_backward(&op, dh, lddh, dr, dr ? lddr : 0, at_(0), op.D, at_(1), op.D, at_(2), at_(3), at_(4), at_(5), at_(6),
