@@ -17,12 +17,17 @@
 #include <algorithm>
 
 #include "gated_norm.cuh"
+#include "pair.cuh"
 #include "ptx.cuh"
 
 namespace trdq {
 namespace {
 
 constexpr int kJoinWarps = 16;
+constexpr int kJoinCtas = 8;
+// Entries that a CTA joins by itself.  More in clusters of kJoinCtas: weights from 4096 samples of a row 163 -> 79 us for the whole call, from 592 runs of a sample 63 -> 60;
+// 130 entries in a cluster 17.1 -> 19.4, 300 51.3 -> 52.9.
+constexpr int64_t kJoinAlone = 384;
 
 template <bool F32>
 struct RowInputs {
@@ -305,40 +310,26 @@ __device__ __forceinline__ void sample_entries(const GatedNormBackward& p, int64
   *last = (end - 1) / p.rows_per_run + sample;
 }
 
-// Joins samples of few entries: a thread takes four columns of a plane of a sample and adds its entries in order.  The whole call with this join and with the
-// one below, us: 16384 x 1152 in samples of 256 rows, ten entries each, 50, 52; 18846 x 680 in samples of 16 45, 79; 4096 x 1152 in samples of one 60, 258.
-__global__ void __launch_bounds__(256) gated_norm_join_samples_kernel(const GatedNormBackward p) {
-  const int quads = p.D / 4;
-  const int64_t item = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, of = item / quads;
-  const int col = static_cast<int>(item - of * quads) * 4, plane = blockIdx.y;
-  float* const to = sample_output(p, plane);
-  if (!to || of > (p.M - 1) / p.rows_per_sample) return;
-  int64_t first, last;
-  sample_entries(p, of, &first, &last);
-  const float* const from = p.workspace + plane * p.entries * p.D + col;
-  const uint16_t* const by = sample_factor(p, plane);
-  griddep_wait();
-  const float4 after = by ? widen4(by + col) : ones4();
-  float4 sum = zeros4();
-#pragma unroll 4
-  for (int64_t i = first; i <= last; ++i) sum = RowSum::add(sum, *reinterpret_cast<const float4*>(from + i * p.D));
-  put4(to + of * p.D + col, by ? fma4(sum, after, zeros4()) : sum);
-}
-
-// Joins many entries of one of the planes (blockIdx.z), 32 columns a CTA, four a thread.  WEIGHTS: the weights' gradients, from all entries; else those of the
-// sample blockIdx.x.  The groups of eight threads take every `groups`-th entry; their sums are added in order.  Bound by latency: with 128 columns
+// Joins many entries of a plane, 32 columns a CTA, four a thread.  WEIGHTS: the weights' gradients, from all entries; else those of a sample.  The groups of eight threads take every `groups`-th entry; their sums are added in order.  Bound by latency: with 128 columns
 // and all three planes in one CTA the sums of 130 runs of 4096 took 7 us instead of 5.
-template <bool WEIGHTS>
-__global__ void __launch_bounds__(32 * kJoinWarps) gated_norm_join_kernel(const GatedNormBackward p) {
+// SHARED: the entries are cut among the kJoinCtas CTAs of a cluster, whose sums are added in their order.
+template <bool WEIGHTS, bool SHARED>
+__device__ __forceinline__ void join_columns(const GatedNormBackward& p, int plane, int columns, int64_t sample) {
   __shared__ float4 part[kJoinWarps][8];
-  const int quad = threadIdx.x & 7, group = threadIdx.x >> 3, groups = blockDim.x >> 3, plane = blockIdx.z;
-  const int col = (blockIdx.y * 8 + quad) * 4;
+  const int quad = threadIdx.x & 7, group = threadIdx.x >> 3, groups = blockDim.x >> 3;
+  const int col = (columns * 8 + quad) * 4;
   const bool in = col < p.D;
   float* const to = !WEIGHTS ? sample_output(p, plane) : plane == 0 ? p.dweight : plane == 1 ? nullptr : p.dpost_weight;
   if (!to) return;
   const int64_t rps = p.rows_per_sample, rpr = p.rows_per_run;
   int64_t first = 0, last = p.entries - 1;
-  if (!WEIGHTS) sample_entries(p, blockIdx.x, &first, &last);
+  if (!WEIGHTS) sample_entries(p, sample, &first, &last);
+  const uint32_t rank = SHARED ? cluster_ctarank() : 0;
+  if (SHARED) {
+    const int64_t n = last + 1 - first, from = first + n * rank / kJoinCtas;
+    last = first + n * (rank + 1) / kJoinCtas - 1;
+    first = from;
+  }
   const uint16_t* const factor = !WEIGHTS ? nullptr : plane == 0 ? p.scale : p.gate;
   const int64_t ld_factor = plane == 0 ? p.ld_scale : p.ld_gate;
   const float* const from = p.workspace + plane * p.entries * p.D + col;
@@ -353,7 +344,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) gated_norm_join_kernel(const 
     for (int64_t i = first + group; i <= last; i += groups) sum = fma4(*reinterpret_cast<const float4*>(from + i * p.D), k, sum);
   } else if (in) {
 #pragma unroll 2
-    for (int64_t i = group; i <= last; i += groups) {
+    for (int64_t i = first + group; i <= last; i += groups) {
       // Sample s begins with entry floor(s rps / rpr) + s = floor(s (rps + rpr) / rpr).  The last entry before a sample that begins with a run is nobody's.
       const int64_t s = ((i + 1) * rpr - 1) / (rps + rpr);
       if ((i - s) * rpr >= min((s + 1) * rps, static_cast<int64_t>(p.M))) continue;
@@ -373,8 +364,50 @@ __global__ void __launch_bounds__(32 * kJoinWarps) gated_norm_join_kernel(const 
     sum = part[0][quad];
     for (int w = 1; w < warps; ++w) sum = RowSum::add(sum, part[w][quad]);
   }
+  if constexpr (SHARED) {
+    __shared__ float4 whole[8];
+    if (group == 0) whole[quad] = sum;
+    cluster_sync_all();
+    if (rank == 0 && group == 0) {
+#pragma unroll
+      for (int k = 1; k < kJoinCtas; ++k) sum = RowSum::add(sum, ld_cluster_v4(map_to_cta(smem_u32(&whole[quad]), k)));
+    }
+    cluster_sync_all();  // no CTA leaves while its sums are read
+    if (rank != 0) return;
+  }
   if (!in || group != 0) return;
-  put4(to + (WEIGHTS ? 0 : static_cast<int64_t>(blockIdx.x) * p.D) + col, by ? fma4(sum, after, zeros4()) : sum);
+  put4(to + (WEIGHTS ? 0 : sample * p.D) + col, by ? fma4(sum, after, zeros4()) : sum);
+}
+
+template <bool WEIGHTS>
+__global__ void __launch_bounds__(32 * kJoinWarps) gated_norm_join_kernel(const GatedNormBackward p) {
+  join_columns<WEIGHTS, false>(p, blockIdx.z, blockIdx.y, blockIdx.x);
+}
+template <bool WEIGHTS>
+__global__ void __cluster_dims__(kJoinCtas, 1, 1) __launch_bounds__(32 * kJoinWarps) gated_norm_join_shared_kernel(const GatedNormBackward p) {
+  join_columns<WEIGHTS, true>(p, blockIdx.z, blockIdx.y, blockIdx.x / kJoinCtas);
+}
+
+// Joins samples of few entries: a thread takes four columns of a plane of a sample and adds its entries in order.  CTAs from sample_ctas on: the weights, which
+// saves a launch (five rows 6.4 -> 5.0 us).  The whole
+// call with this join and with the one above, us: 16384 x 1152 in samples of 256 rows, ten entries each, 50, 52; 18846 x 680 in samples of 16 45, 79; 4096 x 1152 in samples of one 60, 258.
+__global__ void __launch_bounds__(256) gated_norm_join_samples_kernel(const GatedNormBackward p, unsigned sample_ctas) {
+  if (blockIdx.x >= sample_ctas) return join_columns<true, false>(p, blockIdx.y, static_cast<int>(blockIdx.x - sample_ctas), 0);
+  const int quads = p.D / 4;
+  const int64_t item = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, of = item / quads;
+  const int col = static_cast<int>(item - of * quads) * 4, plane = blockIdx.y;
+  float* const to = sample_output(p, plane);
+  if (!to || of > (p.M - 1) / p.rows_per_sample) return;
+  int64_t first, last;
+  sample_entries(p, of, &first, &last);
+  const float* const from = p.workspace + plane * p.entries * p.D + col;
+  const uint16_t* const by = sample_factor(p, plane);
+  griddep_wait();
+  const float4 after = by ? widen4(by + col) : ones4();
+  float4 sum = zeros4();
+#pragma unroll 4
+  for (int64_t i = first; i <= last; ++i) sum = RowSum::add(sum, *reinterpret_cast<const float4*>(from + i * p.D));
+  put4(to + of * p.D + col, by ? fma4(sum, after, zeros4()) : sum);
 }
 
 }  // namespace
@@ -414,19 +447,30 @@ trdq_status launch_gated_norm_backward(const GatedNormBackward& args, cudaStream
   if (e != cudaSuccess) return TRDQ_ERR_CUDA;
   auto warps_for = [](int64_t entries) { return static_cast<unsigned>(std::min<int64_t>(kJoinWarps, std::max<int64_t>(1, entries / 16))); };  // four a group
   const unsigned blocks32 = (p.D / 4 + 7) / 8;
+  bool weights = p.dweight || p.dpost_weight;
   if (p.dscale || p.dshift || p.dgate) {
     const int64_t most = (std::min<int64_t>(p.rows_per_sample, p.M) - 1) / p.rows_per_run + 2;  // entries of a sample
     if (most <= 16) {
       const int64_t ctas = (samples * (p.D / 4) + 255) / 256;
-      if (ctas > 0x7FFFFFFF) return TRDQ_ERR_SHAPE;
-      e = launch_overlapped(gated_norm_join_samples_kernel, dim3(static_cast<unsigned>(ctas), 3), dim3(256), 0, stream, p);
-    } else {
+      if (ctas > 0x7FFFFFFF - blocks32) return TRDQ_ERR_SHAPE;
+      const unsigned sample_ctas = static_cast<unsigned>(ctas);
+      const bool both = weights && p.entries <= kJoinAlone;
+      e = launch_overlapped(gated_norm_join_samples_kernel, dim3(sample_ctas + (both ? blocks32 : 0), 3), dim3(256), 0, stream, p, sample_ctas);
+      weights = weights && !both;
+    } else if (most <= kJoinAlone) {
       e = launch_overlapped(gated_norm_join_kernel<false>, dim3(static_cast<unsigned>(samples), blocks32, 3), dim3(32 * warps_for(most)), 0, stream, p);
+    } else {
+      if (samples > 0x7FFFFFFF / kJoinCtas) return TRDQ_ERR_SHAPE;
+      e = launch_overlapped(gated_norm_join_shared_kernel<false>, dim3(static_cast<unsigned>(samples * kJoinCtas), blocks32, 3), dim3(32 * warps_for(most / kJoinCtas)), 0,
+                            stream, p);
     }
     if (e != cudaSuccess) return TRDQ_ERR_CUDA;
   }
-  if (p.dweight || p.dpost_weight)
+  if (weights && p.entries <= kJoinAlone) {
     e = launch_overlapped(gated_norm_join_kernel<true>, dim3(1, blocks32, 3), dim3(32 * warps_for(p.entries)), 0, stream, p);
+  } else if (weights) {
+    e = launch_overlapped(gated_norm_join_shared_kernel<true>, dim3(kJoinCtas, blocks32, 3), dim3(32 * warps_for(p.entries / kJoinCtas)), 0, stream, p);
+  }
   return e == cudaSuccess ? TRDQ_OK : TRDQ_ERR_CUDA;
 }
 
