@@ -442,6 +442,13 @@ trdq_status trdq_measure_mma_ceiling(int32_t mmas_per_cluster, int32_t* clusters
  * For checking that a stuck pipeline would be reported instead of hanging the GPU. */
 trdq_status trdq_selftest_wait_expiry(void* stream);
 
+/* The same for a whole pipeline: trdq_fp8_linear's kernel of CTA pairs on the given operands (as there, without bias and activation), but with the
+ * copies of its operands left out, so that what waits for them never comes.  The waits expire after a second, the kernel goes through its tiles
+ * without them and ends normally; Y is left with unspecified contents, and the next trdq_device_status reports bit 1 (the MMAs' wait), perhaps bit 2
+ * (the drain's) too.  TRDQ_ERR_SHAPE where the device cannot run that kernel. */
+trdq_status trdq_selftest_fp8_linear_expiry(const uint8_t* codes, const float* scales, int32_t M, int32_t K, const uint8_t* w_codes,
+                                            const float* w_scales, int32_t N, void* Y_bf16, int64_t ldy, void* stream);
+
 /* Library version, major * 100 + minor. */
 int32_t trdq_version(void);
 

@@ -50,6 +50,19 @@ trdq_status check_op(const trdq_gated_norm_op* op) {
   return st;
 }
 
+trdq_status run_fp8_linear(const Fp8Linear& p, bool mute, void* stream) {
+  if (p.M < 0 || p.N <= 0 || p.N % 16 != 0 || !blocks_of_128(p.K)) return TRDQ_ERR_SHAPE;
+  if (p.act != TRDQ_ACT_NONE && p.act != TRDQ_ACT_GELU_TANH) return TRDQ_ERR_SHAPE;
+  if (p.M == 0) return TRDQ_OK;
+  if (!p.codes || !p.scales || !p.w_codes || !p.w_scales || !p.out) return TRDQ_ERR_NULL;
+  if (p.ld < p.N) return TRDQ_ERR_SHAPE;
+  if (p.ld % 8 != 0 || !aligned(p.out, 16) || !aligned(p.codes, 16) || !aligned(p.w_codes, 16) || !aligned(p.scales, 4) || !aligned(p.w_scales, 4) ||
+      !aligned(p.bias_bf16, 8))
+    return TRDQ_ERR_ALIGN;
+  cudaStream_t const cs = static_cast<cudaStream_t>(stream);
+  return finish(mute ? launch_gemm_fp8_pair(p, cs, true) : launch_gemm_fp8(p, cs), stream);
+}
+
 trdq_status run_gated_norm(const trdq_gated_norm_op* op, void* R, int64_t ldr, void* out, int64_t ldo, float* scales, const float* vec,
                            void* stream) {
   if (R) {
@@ -119,16 +132,12 @@ trdq_status trdq_fp8_quantize_weights(const trdq_rotation* rot, int32_t t, const
 
 trdq_status trdq_fp8_linear(const uint8_t* codes, const float* scales, int32_t M, int32_t K, const uint8_t* w_codes, const float* w_scales,
                             int32_t N, const void* bias_bf16, void* Y_bf16, int64_t ldy, int32_t act, void* stream) {
-  if (M < 0 || N <= 0 || N % 16 != 0 || !blocks_of_128(K)) return TRDQ_ERR_SHAPE;
-  if (act != TRDQ_ACT_NONE && act != TRDQ_ACT_GELU_TANH) return TRDQ_ERR_SHAPE;
-  if (M == 0) return TRDQ_OK;
-  if (!codes || !scales || !w_codes || !w_scales || !Y_bf16) return TRDQ_ERR_NULL;
-  if (ldy < N) return TRDQ_ERR_SHAPE;
-  if (ldy % 8 != 0 || !aligned(Y_bf16, 16) || !aligned(codes, 16) || !aligned(w_codes, 16) || !aligned(scales, 4) || !aligned(w_scales, 4) ||
-      !aligned(bias_bf16, 8))
-    return TRDQ_ERR_ALIGN;
-  const Fp8Linear p{codes, scales, w_codes, w_scales, bias_bf16, Y_bf16, ldy, M, N, K, act};
-  return finish(launch_gemm_fp8(p, static_cast<cudaStream_t>(stream)), stream);
+  return run_fp8_linear(Fp8Linear{codes, scales, w_codes, w_scales, bias_bf16, Y_bf16, ldy, M, N, K, act}, false, stream);
+}
+
+trdq_status trdq_selftest_fp8_linear_expiry(const uint8_t* codes, const float* scales, int32_t M, int32_t K, const uint8_t* w_codes,
+                                            const float* w_scales, int32_t N, void* Y_bf16, int64_t ldy, void* stream) {
+  return run_fp8_linear(Fp8Linear{codes, scales, w_codes, w_scales, nullptr, Y_bf16, ldy, M, N, K, TRDQ_ACT_NONE}, true, stream);
 }
 
 trdq_status trdq_gated_norm(const trdq_gated_norm_op* op, void* R, int64_t ldr, void* H_bf16, int64_t ldh, void* stream) {

@@ -113,11 +113,12 @@ __device__ __forceinline__ void tmem_wait_ld_regs(uint32_t (&r)[16]) {
   for (int i = 0; i < 16; ++i) asm volatile("" : "+r"(r[i]));
 }
 
-// Hardware barriers between the warp that waits for the accumulators and the drain, one per accumulator and set.  None is arrived at again before all
-// have passed it: the next arrival follows the accumulator's next MMAs, and those its release.
+// Hardware barrier of a set: the warp that waits for the accumulators and the set's warps meet there once a k-block.  All of them wait (bar.sync), so that
+// none is ever a k-block ahead of the others and the barrier's count stays right whatever became of the mbarriers: also after a wait that expired, when
+// the warp goes through its k-blocks without waiting for them.  (With an arrival that does not wait it would then count several times in one
+// passage, which would end without some of the set's warps and leave those waiting for good.)
 constexpr int kMeet = 32 + 32 * kSetWarps;
-__device__ __forceinline__ void wake_arrive(int acc, int set) { asm volatile("bar.arrive %0, %1;" ::"r"(1 + set * kAccs + acc), "n"(kMeet) : "memory"); }
-__device__ __forceinline__ void wake_wait(int acc, int set) { asm volatile("bar.sync %0, %1;" ::"r"(1 + set * kAccs + acc), "n"(kMeet) : "memory"); }
+__device__ __forceinline__ void meet(int set) { asm volatile("bar.sync %0, %1;" ::"r"(1 + set), "n"(kMeet) : "memory"); }
 
 // Lane and drain warp, read anew from the hardware: not kept in registers from one use to the next.
 struct DrainPlace {
@@ -129,7 +130,8 @@ __device__ __forceinline__ DrainPlace drain_place() {
   return DrainPlace{static_cast<int>(tid & 31), static_cast<int>(tid >> 5) - 4};
 }
 
-template <bool ACT>
+// MUTE: the self-test's form, whose operands are never copied, so that the waits for them expire.
+template <bool ACT, bool MUTE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp8_pair_kernel(const __grid_constant__ Fp8PairParams p) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -215,7 +217,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
         const float scale = __fmul_rn(qx, qw);
         const float2 s2 = make_float2(scale, scale);
         request(kb + 1);
-        wake_wait(acc_idx, set);
+        meet(set);
         tc_fence_after();
         const uint32_t t_row = t_lane + acc_idx * kTileCh;
 #pragma unroll
@@ -281,7 +283,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
     if (warp == 0) {
       // ------------------------------------------------------------------- TMA producer (both CTAs)
-      if (elect_one()) {
+      if (!MUTE && elect_one()) {
         BoundedWaiter w(p.status, kStatusTimeoutProducer);
         const uint32_t leader_full = map_to_cta(bar_full, 0);
         Ring st;
@@ -331,7 +333,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
         for (int kb = 0; kb < p.num_kb; ++kb) {
           if (lane == 0) w.wait(bar_tfull + 8 * acc.idx, acc.phase);
           __syncwarp();
-          wake_arrive(acc.idx, set);
+          meet(set);
           acc.advance(kAccs);
         }
         set ^= 1;
@@ -351,6 +353,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_fp
   }
 }
 
+// The register split draws on what the launch allocates.
+bool can_run(void (*kernel)(Fp8PairParams)) {
+  cudaFuncAttributes attr;
+  return cudaFuncGetAttributes(&attr, kernel) == cudaSuccess && attr.numRegs == kRegsLaunch &&
+         cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) == cudaSuccess;
+}
+
 }  // namespace
 
 // Clusters of two CTAs that can be resident at once; 0: the kernel cannot run here.
@@ -358,29 +367,23 @@ int fp8_pair_clusters(int dev) {
   static PerDevice<int> cached;
   int known = cached.get(dev);
   if (known != 0) return known > 0 ? known : 0;
-  bool ok = true;
-  for (const auto kernel : {gemm_fp8_pair_kernel<false>, gemm_fp8_pair_kernel<true>}) {
-    cudaFuncAttributes attr;
-    // the register split draws on what the launch allocates
-    ok = ok && cudaFuncGetAttributes(&attr, kernel) == cudaSuccess && attr.numRegs == kRegsLaunch &&
-         cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) == cudaSuccess;
-  }
+  bool ok = can_run(gemm_fp8_pair_kernel<false, false>) && can_run(gemm_fp8_pair_kernel<true, false>);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2);
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = kSmemBytes;
   int n = 0;
-  ok = ok && cudaOccupancyMaxActiveClusters(&n, gemm_fp8_pair_kernel<false>, &cfg) == cudaSuccess && n > 0;
+  ok = ok && cudaOccupancyMaxActiveClusters(&n, gemm_fp8_pair_kernel<false, false>, &cfg) == cudaSuccess && n > 0;
   if (!ok) cudaGetLastError();
   cached.set(dev, ok ? n : -1);
   return ok ? n : 0;
 }
 
-trdq_status launch_gemm_fp8_pair(const Fp8Linear& a, cudaStream_t stream) {
+trdq_status launch_gemm_fp8_pair(const Fp8Linear& a, cudaStream_t stream, bool mute) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return TRDQ_ERR_CUDA;
   const int resident = fp8_pair_clusters(dev);
-  if (resident == 0) return TRDQ_ERR_SHAPE;
+  if (resident == 0 || (mute && !can_run(gemm_fp8_pair_kernel<false, true>))) return TRDQ_ERR_SHAPE;
   Fp8PairParams p;
   trdq_status st = encode_tmap_u8_sw128(&p.tmap_a, a.codes, a.K, a.M, a.K, kTileK, kTileM);
   if (st == TRDQ_OK) st = encode_tmap_u8_sw128(&p.tmap_b, a.w_codes, a.K, a.N, a.K, kTileK, kTileCh / 2);
@@ -401,8 +404,8 @@ trdq_status launch_gemm_fp8_pair(const Fp8Linear& a, cudaStream_t stream) {
   p.status = device_status_word();
   if (!p.status) return TRDQ_ERR_CUDA;
   const int clusters = static_cast<int>(total < resident ? total : resident);
-  const cudaError_t e = launch_overlapped(a.act ? gemm_fp8_pair_kernel<true> : gemm_fp8_pair_kernel<false>, dim3(2 * clusters), dim3(kThreads), kSmemBytes,
-                                          stream, p);
+  const auto kernel = mute ? gemm_fp8_pair_kernel<false, true> : a.act ? gemm_fp8_pair_kernel<true, false> : gemm_fp8_pair_kernel<false, false>;
+  const cudaError_t e = launch_overlapped(kernel, dim3(2 * clusters), dim3(kThreads), kSmemBytes, stream, p);
   return e == cudaSuccess ? TRDQ_OK : TRDQ_ERR_CUDA;
 }
 

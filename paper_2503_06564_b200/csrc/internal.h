@@ -184,7 +184,8 @@ trdq_status launch_gemm_fp8(const Fp8Linear& p, cudaStream_t stream);
 // gemm_fp8_2cta.cu: the CTA-pair kernel, and how many pairs of CTAs the device holds at once (0: it cannot run there; also when the compiler gave it other
 // registers than its split needs)
 int fp8_pair_clusters(int device);
-trdq_status launch_gemm_fp8_pair(const Fp8Linear& p, cudaStream_t stream);
+// mute: the self-test of its waits
+trdq_status launch_gemm_fp8_pair(const Fp8Linear& p, cudaStream_t stream, bool mute = false);
 
 // gated_norm.cu, gated_norm_backward.cu: the fields of trdq_gated_norm_op as the kernels take them
 struct GatedNorm {

@@ -34,7 +34,7 @@ EXPORTS = (
     "trdq_selftest_wait_expiry", "trdq_rotation_create_dense", "trdq_rotate_dense_workspace", "trdq_rotate_dense_quantize",
     "trdq_greedy_rotation_block", "trdq_linear_act", "trdq_norm_rotate_quantize", "trdq_kernel_choice",
     "trdq_measure_mma_ceiling", "trdq_fp8_quantize", "trdq_fp8_quantize_weights", "trdq_fp8_linear", "trdq_gated_norm", "trdq_gated_norm_fp8",
-    "trdq_gated_norm_backward_workspace", "trdq_gated_norm_backward",
+    "trdq_gated_norm_backward_workspace", "trdq_gated_norm_backward", "trdq_selftest_fp8_linear_expiry",
 )
 
 
@@ -114,6 +114,7 @@ def lib() -> C.CDLL:
         l.trdq_fp8_quantize.argtypes = [vp, i32, vp, i64, i32, i32, vp, vp, vp]
         l.trdq_fp8_quantize_weights.argtypes = [vp, i32, vp, i32, i32, vp, vp, vp]
         l.trdq_fp8_linear.argtypes = [vp, vp, i32, i32, vp, vp, i32, vp, vp, i64, i32, vp]
+        l.trdq_selftest_fp8_linear_expiry.argtypes = [vp, vp, i32, i32, vp, vp, i32, vp, i64, vp]
         l.trdq_gated_norm.argtypes = [op, vp, i64, vp, i64, vp]
         l.trdq_gated_norm_fp8.argtypes = [op, vp, i32, vp, i64, vp, vp, vp]
         l.trdq_gated_norm_backward_workspace.argtypes = [op, C.POINTER(C.c_uint64)]
@@ -826,6 +827,21 @@ def trdq_measure_mma_ceiling(mmas_per_cluster: int) -> int:
 def trdq_selftest_wait_expiry() -> None:
     """Launches the kernel whose only barrier is never signalled (its wait expires after 20 ms)."""
     _check(lib().trdq_selftest_wait_expiry(_stream()), "trdq_selftest_wait_expiry")
+
+
+def trdq_selftest_fp8_linear_expiry(codes, scales, w_codes, w_scales) -> None:
+    """Launches the block-scaled product's kernel of CTA pairs without the copies of its operands (its waits expire after a second)."""
+    import torch
+    M, K, N = int(codes.shape[0]), int(codes.shape[1]), int(w_codes.shape[0])
+    where = "trdq_selftest_fp8_linear_expiry"
+    _here(where, codes, scales, w_codes, w_scales)
+    _expect(where, codes, (M, K), *_fp8_types())
+    _expect(where, scales, (K // 128, M), torch.float32)
+    _expect(where, w_codes, (N, K), *_fp8_types())
+    _expect(where, w_scales, ((N + 127) // 128, K // 128), torch.float32)
+    _whole(where, codes, scales, w_codes, w_scales)
+    out = torch.empty((M, N), dtype=torch.bfloat16, device=codes.device)
+    _check(lib().trdq_selftest_fp8_linear_expiry(_ptr(codes), _ptr(scales), M, K, _ptr(w_codes), _ptr(w_scales), N, _ptr(out), N, _stream()), where)
 
 
 def trdq_device_status() -> int:
