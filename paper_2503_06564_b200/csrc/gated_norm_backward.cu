@@ -410,6 +410,22 @@ __global__ void __launch_bounds__(256) gated_norm_join_samples_kernel(const Gate
   put4(to + of * p.D + col, by ? fma4(sum, after, zeros4()) : sum);
 }
 
+// Two chunks a thread.  What the kernel may ask for is state of the function on its device, which calls of other widths share, from other threads too: it
+// is set once, to what the widest rows take.
+template <bool F32>
+cudaError_t launch_wide(const GatedNormBackward& p, dim3 grid, dim3 threads, cudaStream_t stream) {
+  constexpr size_t kThreadBytes = sizeof(float4) * 2 * kLocalPieces<F32>;
+  static PerDeviceFlag configured;
+  const auto kernel = gated_norm_backward_kernel<2, F32, true>;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && !configured.get(dev)) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kThreadBytes * 32 * kRowWarps));
+    if (e == cudaSuccess) configured.set(dev, true);
+  }
+  return e != cudaSuccess ? e : launch_overlapped(kernel, grid, threads, kThreadBytes * threads.x, stream, p);
+}
+
 }  // namespace
 
 // Whether the kernel with less in registers holds more CTAs of the width.  us, without and with it: 16384 x 1152 56.2, 52.3; 16384 x 2560 148.5, 107.6;
@@ -434,11 +450,7 @@ trdq_status launch_gated_norm_backward(const GatedNormBackward& args, cudaStream
   const dim3 g(static_cast<unsigned>(grid)), t(threads);
   cudaError_t e;
   if (row_chunks(p.D) == 2) {
-    const auto kernel = p.f32 ? gated_norm_backward_kernel<2, true, true> : gated_norm_backward_kernel<2, false, true>;
-    const size_t bytes = sizeof(float4) * 2 * (p.f32 ? kLocalPieces<true> : kLocalPieces<false>) * threads;
-    // (on each call: the attribute belongs to the device)
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)) != cudaSuccess) return TRDQ_ERR_CUDA;
-    e = launch_overlapped(kernel, g, t, bytes, stream, p);
+    e = p.f32 ? launch_wide<true>(p, g, t, stream) : launch_wide<false>(p, g, t, stream);
   } else if (keeps_local(threads, p.f32)) {
     e = launch_overlapped(gated_norm_backward_kernel<1, false, true>, g, t, sizeof(float4) * kLocalPieces<false> * threads, stream, p);
   } else {
