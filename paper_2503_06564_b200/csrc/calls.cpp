@@ -438,10 +438,12 @@ bool real(PyObject* o, float* out) {
 
 // The arguments that the three norm calls share: X, branch, gate, shift, scale, weight, post_weight, norm, post_norm, rows_per_sample, eps, res_scale
 constexpr int kNormArgs = 12;
-bool norm_op(PyObject* const* a, c10::DeviceIndex device, trdq_gated_norm_op* op, int64_t* samples) {
+bool norm_op(PyObject* const* a, c10::DeviceIndex* current, trdq_gated_norm_op* op, int64_t* samples) {
   if (!plain(a[0])) return false;
   for (int i = 1; i < 7; ++i)
     if (!plain_or_none(a[i])) return false;
+  // (asked for behind the first CUDA tensor: without a device the question itself is an error, and not the one that the general way reports)
+  const c10::DeviceIndex device = *current = c10::cuda::current_device();
   const at::Tensor& x = tensor(a[0]);
   if (x.dim() != 2 || (x.scalar_type() != at::kBFloat16 && x.scalar_type() != at::kFloat) || !int32_size(x.size(0)) || !int32_size(x.size(1))) return false;
   const int64_t M = x.size(0), D = x.size(1);
@@ -490,8 +492,8 @@ PyObject* gated_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   trdq_gated_norm_op op;
   int64_t samples, ldr, ldh;
-  const c10::DeviceIndex device = c10::cuda::current_device();
-  GENERAL_WAY_UNLESS(n == kNormArgs + 2 && norm_op(a, device, &op, &samples) && no_modes());
+  c10::DeviceIndex device;
+  GENERAL_WAY_UNLESS(n == kNormArgs + 2 && norm_op(a, &device, &op, &samples) && no_modes());
   const at::ScalarType type = op.stream_f32 ? at::kFloat : at::kBFloat16;
   GENERAL_WAY_UNLESS(norm_output(a[12], op, type, device, &ldr) && norm_output(a[13], op, at::kBFloat16, device, &ldh));
   Outputs out(a[0]);
@@ -509,8 +511,8 @@ PyObject* gated_norm_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) {
   int64_t samples, ldr, ldc;
   void* rot;
   int32_t t;
-  const c10::DeviceIndex device = c10::cuda::current_device();
-  GENERAL_WAY_UNLESS(n == kNormArgs + 5 && norm_op(a, device, &op, &samples) && handle_or_none(a[12], &rot) && number(a[13], &t) && no_modes());
+  c10::DeviceIndex device;
+  GENERAL_WAY_UNLESS(n == kNormArgs + 5 && norm_op(a, &device, &op, &samples) && handle_or_none(a[12], &rot) && number(a[13], &t) && no_modes());
   const at::ScalarType type = op.stream_f32 ? at::kFloat : at::kBFloat16;
   GENERAL_WAY_UNLESS(norm_output(a[14], op, type, device, &ldr) && norm_output(a[15], op, at::kFloat8_e4m3fn, device, &ldc) && ldc == op.D);
   GENERAL_WAY_UNLESS(a[16] == Py_None || (plain(a[16]) && on_device(tensor(a[16]), device) && tensor(a[16]).scalar_type() == at::kFloat &&
@@ -531,8 +533,8 @@ PyObject* gated_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   trdq_gated_norm_op op;
   int64_t samples, lddh, lddr;
-  const c10::DeviceIndex device = c10::cuda::current_device();
-  GENERAL_WAY_UNLESS(n == kNormArgs + 2 && norm_op(a, device, &op, &samples) && no_modes());
+  c10::DeviceIndex device;
+  GENERAL_WAY_UNLESS(n == kNormArgs + 2 && norm_op(a, &device, &op, &samples) && no_modes());
   const at::ScalarType type = op.stream_f32 ? at::kFloat : at::kBFloat16;
   GENERAL_WAY_UNLESS(a[12] != Py_None && norm_output(a[12], op, at::kBFloat16, device, &lddh) && norm_output(a[13], op, type, device, &lddr));
   uint64_t bytes = 0;
