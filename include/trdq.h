@@ -422,7 +422,8 @@ trdq_status trdq_device_status(uint32_t* word);
 
 /* Reports which kernel a call would run on the current device, for benchmark and profile reports (the paper has no
  * counterpart).  stage 0: trdq_rotate_quantize on M rows of K channels (N, wbits ignored); stage 1: trdq_linear on M rows
- * against [N, K] weights of `wbits` bits.  `name` (host, at least 48 bytes, `name_bytes` its size) receives a
+ * against [N, K] weights of `wbits` bits; stage 2: trdq_fp8_linear on M rows against [N, K] weights (wbits ignored), with the tokens of a tile, the
+ * CTAs that share one and the CTAs an SM where the kernel has a choice of them.  `name` (host, at least 48 bytes, `name_bytes` its size) receives a
  * NUL-terminated kernel name such as "gemm_w8a8_pair_kernel<256>".  The answer comes from the same functions the
  * launchers use.  TRDQ_ERR_CUDA without a device: the choice depends on its SM count. */
 trdq_status trdq_kernel_choice(int32_t stage, int32_t M, int32_t K, int32_t N, int32_t wbits, char* name, int32_t name_bytes);

@@ -735,6 +735,11 @@ trdq_status trdq_kernel_choice(int32_t stage, int32_t M, int32_t K, int32_t N, i
     describe_rotate_quantize_kernel(M, K, name, static_cast<size_t>(name_bytes));
     return TRDQ_OK;
   }
+  if (stage == 2) {
+    if (N <= 0 || N % 16 != 0) return TRDQ_ERR_SHAPE;
+    describe_gemm_fp8_kernel(M, K, N, dev, name, static_cast<size_t>(name_bytes));
+    return TRDQ_OK;
+  }
   if (stage != 1 || N <= 0) return TRDQ_ERR_SHAPE;
   if (wbits != 8 && wbits != 4) return TRDQ_ERR_WBITS;
   describe_gemm_kernel(M, K, N, wbits, name, static_cast<size_t>(name_bytes));

@@ -22,6 +22,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdio>
 
 #include "epilogue.cuh"
 #include "internal.h"
@@ -306,7 +307,7 @@ int resident_clusters(int dev, int log_splits) {
   return ok ? n : 0;
 }
 
-// How a call is cut: the tokens of a tile, the CTAs that share a tile's k-blocks, the CTAs an SM.  us: its expected time.
+// How a call is cut: the tokens of a tile (0: the pair kernel), the CTAs that share a tile's k-blocks, the CTAs an SM.  us: its expected time.
 struct Cut {
   int tokens = 0, log_splits = 0, per_sm = 1;
   double us = HUGE_VAL;
@@ -377,9 +378,7 @@ trdq_status launch_tokens(const Fp8Linear& a, const Cut& cut, cudaStream_t strea
 // Few rows go to the kernel above, in the cheapest cut; the pair kernel (tiles of 256 rows and 128 columns, 0.28 us a k-block, no cut of K) takes over where
 // it is expected to be faster.  Measured, us, this kernel against the pair's: 64 x 4096 x 16384 17.3, 25; 256 x 4608 x 1152 10.0, 12.8;
 // 128 x 4096 x 16384 22, 29; 256 x 4096 x 4096 13.8, 12.3; 256 x 4096 x 16384 42, 25.
-trdq_status launch_gemm_fp8(const Fp8Linear& a, cudaStream_t stream) {
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return TRDQ_ERR_CUDA;
+static Cut choose(const Fp8Linear& a, int dev) {
   const int pairs = fp8_pair_clusters(dev);
   const int64_t rounds = pairs > 0 ? (tiles_of(a, 256, 128) + pairs - 1) / pairs : 0;
   Cut cut;
@@ -389,11 +388,29 @@ trdq_status launch_gemm_fp8(const Fp8Linear& a, cudaStream_t stream) {
     consider<32>(a, dev, cut);
     consider<64>(a, dev, cut);
   }
+  return cut;
+}
+
+void describe_gemm_fp8_kernel(int32_t M, int32_t K, int32_t N, int dev, char* name, size_t bytes) {
+  Fp8Linear a = {};
+  a.M = M, a.K = K, a.N = N;
+  const Cut cut = choose(a, dev);
+  if (cut.tokens == 0) {
+    snprintf(name, bytes, "gemm_fp8_pair_kernel");
+  } else {
+    snprintf(name, bytes, "gemm_fp8_kernel<%d>, %d a cluster, %d an SM", cut.tokens, 1 << cut.log_splits, cut.per_sm);
+  }
+}
+
+trdq_status launch_gemm_fp8(const Fp8Linear& a, cudaStream_t stream) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return TRDQ_ERR_CUDA;
+  const Cut cut = choose(a, dev);
   switch (cut.tokens) {
     case 16: return launch_tokens<16>(a, cut, stream);
     case 32: return launch_tokens<32>(a, cut, stream);
     case 64: return launch_tokens<64>(a, cut, stream);
-    default: return pairs > 0 ? launch_gemm_fp8_pair(a, stream) : TRDQ_ERR_CUDA;
+    default: return fp8_pair_clusters(dev) > 0 ? launch_gemm_fp8_pair(a, stream) : TRDQ_ERR_CUDA;
   }
 }
 

@@ -811,7 +811,7 @@ def trdq_run_layers(layers: LayerList, t: int, first: int = 0, count: Optional[i
 
 
 def trdq_kernel_choice(stage: int, M: int, K: int, N: int = 0, wbits: int = 8) -> str:
-    """Name of the kernel trdq_rotate_quantize (stage 0) or trdq_linear (stage 1) runs for this shape on the current device."""
+    """Name of the kernel trdq_rotate_quantize (stage 0), trdq_linear (stage 1) or trdq_fp8_linear (stage 2) runs for this shape on the current device."""
     buf = C.create_string_buffer(96)
     _check(lib().trdq_kernel_choice(int(stage), int(M), int(K), int(N), int(wbits), buf, 96), "trdq_kernel_choice")
     return buf.value.decode()
