@@ -317,9 +317,10 @@ int64_t tiles_of(const Fp8Linear& a, int tokens, int channels) {
   return ((static_cast<int64_t>(a.M) + tokens - 1) / tokens) * ((static_cast<int64_t>(a.N) + channels - 1) / channels);
 }
 
-// The times are lines through those measured (8 to 256 rows, 9 to 64 k-blocks, 9 to 128 column tiles; most within 15 % of them): a call's fixed part,
-// what joining a cluster's sums adds, and the k-blocks that the busiest CTA goes through at the pace of a CTA that has its SM (us_alone) or shares it
-// (us_shared).  CTAs that have to wait for others to leave cost their start as well.
+// The times are lines through those measured (8 to 256 rows, 9 to 64 k-blocks, 9 to 128 column tiles; most within 15 % of them, but for calls that the weights' bytes
+// bound): a call's fixed part, what joining a cluster's sums adds, and the k-blocks that the busiest CTA goes through at the pace of a CTA that has its SM
+// (us_alone) or shares it (us_shared).  CTAs that have to wait for others to leave cost their start as well.  The weights' bytes are in none of the lines: every
+// cut reads them once, so a call that they bound takes longer than expected (1 x 4096 x 16384 14.4 us for 9.0; 10.2 of it the 67 MB) whichever it gets.
 template <int T>
 void consider(const Fp8Linear& a, int dev, Cut& best) {
   constexpr double us_alone = T == 16 ? 0.21 : T == 32 ? 0.25 : 0.315, us_shared = T == 16 ? 0.38 : T == 32 ? 0.45 : 0.65, us_fixed = T == 64 ? 3.4 : 2.3;
@@ -377,17 +378,16 @@ trdq_status launch_tokens(const Fp8Linear& a, const Cut& cut, cudaStream_t strea
 
 // Few rows go to the kernel above, in the cheapest cut; the pair kernel (tiles of 256 rows and 128 columns, 0.28 us a k-block, no cut of K) takes over where
 // it is expected to be faster.  Measured, us, this kernel against the pair's: 64 x 4096 x 16384 17.3, 25; 256 x 4608 x 1152 10.0, 12.8;
-// 128 x 4096 x 16384 22, 29; 256 x 4096 x 4096 13.8, 12.3; 256 x 4096 x 16384 42, 25.
+// 128 x 4096 x 16384 22, 29; 256 x 4096 x 4096 13.8, 12.3; 256 x 4096 x 16384 42, 25; wide outputs, where the pair kernel has many rounds of tiles that are
+// nearly empty of rows: 1 x 4096 x 65536 47, 221; 64 x 4096 x 65536 54, 77; 64 x 4096 x 131072 106, 142.
 static Cut choose(const Fp8Linear& a, int dev) {
   const int pairs = fp8_pair_clusters(dev);
   const int64_t rounds = pairs > 0 ? (tiles_of(a, 256, 128) + pairs - 1) / pairs : 0;
   Cut cut;
   if (pairs > 0) cut.us = (rounds > 1 ? 6.0 : 4.0) + static_cast<double>(rounds) * (a.K / kTileK * 0.28 + 0.3);
-  if (pairs == 0 || rounds <= 4) {  // beyond four rounds of the pair kernel the cuts are only slower
-    consider<16>(a, dev, cut);
-    consider<32>(a, dev, cut);
-    consider<64>(a, dev, cut);
-  }
+  consider<16>(a, dev, cut);
+  consider<32>(a, dev, cut);
+  consider<64>(a, dev, cut);
   return cut;
 }
 

@@ -13,7 +13,10 @@ FORMS = [
     ((32, 1, 1), 1500, 144, 128), ((32, 1, 2), 65, 8192, 128), ((32, 2, 1), 65, 2048, 2048), ((32, 2, 2), 17, 16384, 4608), ((32, 4, 1), 700, 16, 1152),
     ((32, 4, 2), 65, 2048, 4096), ((32, 8, 1), 300, 16, 4096), ((32, 8, 2), 17, 2304, 8192),
     ((64, 1, 1), 65, 8192, 1152), ((64, 1, 2), 129, 8192, 128), ((64, 2, 1), 1500, 144, 4096), ((64, 4, 1), 1500, 16, 4608), ((64, 8, 1), 512, 16, 16384),
-    ((64, 8, 2), 300, 2048, 65536), (PAIR, 300, 4608, 384), (PAIR, 4096, 512, 384), (PAIR, 2057, 4624, 1152),
+    ((64, 8, 2), 300, 2048, 65536),
+    # few rows against a wide matrix, whose tiles are many rounds of the pairs: the rows decide
+    ((16, 1, 2), 1, 65536, 1152), ((32, 1, 2), 17, 40000, 1152), ((64, 2, 2), 64, 49152, 4096), (PAIR, 128, 65536, 1152),
+    (PAIR, 300, 4608, 384), (PAIR, 4096, 512, 384), (PAIR, 2057, 4624, 1152),
 ]
 
 
