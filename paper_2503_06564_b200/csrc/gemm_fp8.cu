@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(Cfg<T>::kThreads, 2) gemm_fp8_kernel(const __g
       w.settle();
     }
   } else if (warp == 2) {
-    BoundedWaiter w(p.status, kStatusTimeoutUnpack);
+    BoundedWaiter w(p.status, kStatusTimeoutScales);
     Ring slot;
     for (int kb = kb0; kb < kb1; ++kb) {
       w.wait(bar_tempty + 8 * slot.idx, slot.phase ^ 1);

@@ -12,6 +12,7 @@ enum : uint32_t {
   kStatusTimeoutMma = 1u << 1,       // MMA issuer gave up waiting for data or a free accumulator
   kStatusTimeoutEpilogue = 1u << 2,  // epilogue gave up waiting for an accumulator
   kStatusTimeoutUnpack = 1u << 3,    // int4 unpack warps gave up waiting
+  kStatusTimeoutScales = 1u << 4,    // the warp that copies the tokens' scales of a k-block gave up waiting for a free slot
   kStatusTimeoutSelfTest = 1u << 31, // the self-test's deliberately unsignalled barrier
 };
 
