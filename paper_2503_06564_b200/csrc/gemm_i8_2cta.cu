@@ -518,7 +518,11 @@ int pair_tile_choice(int64_t tiles_m, int N, int dev, int* clusters_out) {
 // ceiling any GEMM built on the instruction can approach on the device at its current clocks.
 // ---------------------------------------------------------------------------------------------
 constexpr int kCeilingThreads = 128;
-constexpr int kCeilingSmemBytes = 1024 + 2 * kTileM * kTileKBytes + 64;
+// All of an SM's shared memory, of which it uses the first 33 KB: no other CTA with tensor memory may share the SM.  A pair holds all 512 columns and waits
+// for its peer; beside it a cluster of gemm_fp8.cu (two CTAs an SM, 128 or 256 columns each, which wait for one another too) could hold columns on one SM that
+// the pair waits for and wait for columns on another that the pair holds, and neither would end.
+constexpr int kCeilingSmemBytes = kSmemBudget;
+static_assert(1024 + 2 * kTileM * kTileKBytes + 64 <= kCeilingSmemBytes, "operands and barriers");
 
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCeilingThreads, 1) mma_ceiling_kernel(int mmas, uint32_t* status) {
   extern __shared__ uint8_t smem_raw[];
