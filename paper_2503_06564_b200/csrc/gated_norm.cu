@@ -11,6 +11,8 @@
 // 128-block of the rotation: three butterfly stages in a thread, four by shuffle, in the order h = 1, 2, ..., 64 of the other kernels.
 // What bounds it: memory, 8 bytes a channel with a bf16 stream, 7 with codes, and close behind it instruction issue.  32768 x 1152 (adaLN, bf16) 55 us, 5.5 TB/s of
 // a measured 6.6; 8190 x 1152 to codes 22 us, issue alone (0.63 a clock and scheduler beside packed operations of two; without rotation and quantizer 15 us).
+// More than 4096 channels, 4096 x 8192: bf16 52 us, fp32 stream 75, bf16 to codes 69, fp32 to codes 125; with an fp32 stream the 128 registers do not hold two chunks (40 bytes of
+// a thread spill, 96 with codes).
 // Measured and not better: two rows a step with one barrier (122 registers, 61 us); two rows that meet inside a warp where D is an odd multiple of 128 (65 us); groups
 // of rows in a CTA with barriers of their own; 16 channels a thread (61 us); the inputs of two or three rows ahead in shared memory (55 us, codes 24 us).
 #include <algorithm>

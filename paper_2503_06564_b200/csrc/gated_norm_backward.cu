@@ -12,7 +12,7 @@
 // end of the run, the sums go to the workspace, run c's of sample s to entry c + s (each step along the rows moves to the next run, the
 // next sample or both, so no entry is used twice).  A second kernel joins them in a fixed order: equal inputs give equal gradients.  The statistics are taken again from r and b, which are in registers for the gradient itself.
 // What bounds it: the latencies of three row sums a row with as many rows in flight as registers allow, beside memory, 12 bytes a channel with a bf16 stream.
-// 16384 x 1152 (adaLN) 50 us, 4.5 TB/s of a measured 6.6, 44 without the parameters' gradients; 517 x 4096 (fp32 stream, both norms) 17.5 us.
+// 16384 x 1152 (adaLN) 50 us, 4.5 TB/s of a measured 6.6, 45 without the parameters' gradients; 517 x 4096 (fp32 stream, both norms) 17.5 us.
 // Measured and not better: the row sums in two rounds in place of three or four (registers spill: 63 us).
 #include <algorithm>
 
@@ -40,7 +40,8 @@ __device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wai
 
 // What a thread keeps between rows besides its sums: its columns' two parameters, and the inputs of the next row, which are on their way while this row is
 // computed.  In registers (LOCAL false), or in 16-byte pieces of shared memory that no other thread touches, `step` threads apart (LOCAL true): with one chunk a
-// thread 96 registers instead of 128, so five warps a scheduler and not four; with two, what else would spill.
+// thread 96 registers instead of 128, so five warps a scheduler and not four; with two, most of what would spill (2048 x 8192 113 -> 72 us; 152 bytes of a thread still
+// do, 176 with an fp32 stream, which takes 113).
 template <bool F32, bool LOCAL>
 struct Kept;
 template <bool F32>

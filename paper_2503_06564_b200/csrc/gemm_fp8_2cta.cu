@@ -8,14 +8,17 @@
 //   warp 2       waits for the accumulators' mbarriers and wakes the drain through hardware barriers
 //   warps 4-19   drain: two sets of eight warps that take every second tile.  A thread owns one row and 64 columns, its scale is one number a
 //                k-block; at the end of a tile bias, activation, bf16, staging tile, TMA store, while the other set adds up the next tile.
-// Synchronisation as in gemm_i8_2cta.cu, with the accumulator barriers per k-block; every wait bounded.
+// Synchronisation as in gemm_i8_2cta.cu, with the accumulator barriers per k-block.  Every wait for an mbarrier is bounded; the hardware barriers have no limit, but
+// the warps that meet at one all come to it equally often, whatever became of the mbarriers.
 //
-// What bounds it: operand delivery from L2 (24 KB a CTA and k-block, 11 TB/s over the SMs), close behind it the drain.  Beside MMAs and copies a
+// What bounds it: operand delivery from L2 (24 KB a CTA and k-block, 11 TB/s over the SMs; 9 in a steady load, where the power limit lowers the clocks:
+// 32768 x 1152 x 4608 takes 190 us by itself and 225 to 235 back to back), close behind it the drain.  Beside MMAs and copies a
 // shared-memory access of another warp is slow, an mbarrier wait that is over takes 70 to 200 clocks, against 256 clocks of MMA and 130 of multiply-adds
 // for a k-block.  So one warp waits for all, and hardware barriers (20 clocks) pass it on; and the scales are requested ahead (the row's line fetched
 // only a k-block before its use, the round trip set the pace: 32768 x 1152 x 4608 219 us in place of 187, 4096 x 1152 x 4608 32 in place of 28).
-// M x N x K, microseconds with one set of drain warps -> two: 4096 x 4608 x 1152 33 -> 28, 2057 x 4624 x 1152 21 -> 18, 16384 x 3456 x 1152 84 -> 73;
-// long reductions 32768 x 1152 x 4608 178 -> 187, 8192 x 4096 x 4096 140 -> 139.
+// M x N x K, microseconds by itself with one set of drain warps -> two: 4096 x 4608 x 1152 33 -> 28, 2057 x 4624 x 1152 21 -> 18, 16384 x 3456 x 1152 84 -> 73;
+// long reductions 32768 x 1152 x 4608 178 -> 187, 8192 x 4096 x 4096 140 -> 139.  Two for every length: one form, which costs the long reductions up to 5 %.
+// (Since the waiting warp meets the drain in place of leaving word for it: 16384 x 3456 x 1152 74, 32768 x 1152 x 4608 190, 8192 x 4096 x 4096 138.)
 // Measured and not better: tiles of 256 x 256, which need 2/3 of the operand bytes but leave tensor memory two accumulators and a thread 128 sums
 // (1040 clocks a k-block in place of 512: the hand-over MMA - commit - wait - loads - release - wait is longer than the MMAs of the other accumulator;
 // 32768 x 1152 x 4608 189, 4096 x 1152 x 4608 36, 8192 x 4096 x 4096 131); the same with each 128-column half handed over by itself and sixteen drain
