@@ -301,8 +301,9 @@ trdq_status trdq_greedy_rotation_block(const float* x_calib, int32_t rows, int32
  * so that v is close to scale * code.  A block is 128 consecutive channels of one row for activations and 128 x 128 for weights.  The
  * rotation's block (Eq. 8) is the scale's block, so v may be the rotated row of Eq. 10, G_t(X) or H_t(W), without a pass of its own:
  * with both sides rotated by the same object and time-step the product is that of trdq_linear.  These calls take the codes and scales
- * as plain device arrays, which do not know their rotation: weights quantized at t serve the time-steps of t's group only, a program that passes through
- * all groups keeps a set for each (trdq_group_of), and with the wrong one the product is wrong without an error; 128 x 128-scaled e4m3 weights that come from elsewhere are used as they are.
+ * as plain device arrays, which do not know their rotation: weights quantized at t serve the time-steps of t's group only, a program that
+ * passes through all groups keeps a set for each (trdq_group_of), and with the wrong one the product is wrong without an error.
+ * 128 x 128-scaled e4m3 weights that come from elsewhere are used as they are.
  * A NaN or an infinity in X spoils its own row of the product, which becomes NaN, and no other row.
  *
  * trdq_fp8_quantize: X_bf16 dev [M, ldx] (ldx >= K, ldx % 8 == 0, 16-byte aligned); codes: dev e4m3 [M, K], 16-byte aligned; scales: dev fp32

@@ -736,9 +736,8 @@ trdq_status trdq_kernel_choice(int32_t stage, int32_t M, int32_t K, int32_t N, i
     return TRDQ_OK;
   }
   if (stage == 2) {
-    if (N <= 0 || N % 16 != 0) return TRDQ_ERR_SHAPE;
-    describe_gemm_fp8_kernel(M, K, N, dev, name, static_cast<size_t>(name_bytes));
-    return TRDQ_OK;
+    if (N <= 0 || N % 16 != 0 || K > TRDQ_MAX_K) return TRDQ_ERR_SHAPE;
+    return describe_gemm_fp8_kernel(M, K, N, dev, name, static_cast<size_t>(name_bytes));
   }
   if (stage != 1 || N <= 0) return TRDQ_ERR_SHAPE;
   if (wbits != 8 && wbits != 4) return TRDQ_ERR_WBITS;

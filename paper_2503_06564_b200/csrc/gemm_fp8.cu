@@ -391,15 +391,18 @@ static Cut choose(const Fp8Linear& a, int dev) {
   return cut;
 }
 
-void describe_gemm_fp8_kernel(int32_t M, int32_t K, int32_t N, int dev, char* name, size_t bytes) {
+trdq_status describe_gemm_fp8_kernel(int32_t M, int32_t K, int32_t N, int dev, char* name, size_t bytes) {
   Fp8Linear a = {};
   a.M = M, a.K = K, a.N = N;
   const Cut cut = choose(a, dev);
-  if (cut.tokens == 0) {
+  if (cut.tokens > 0) {
+    snprintf(name, bytes, "gemm_fp8_kernel<%d>, %d a cluster, %d an SM", cut.tokens, 1 << cut.log_splits, cut.per_sm);
+  } else if (fp8_pair_clusters(dev) > 0) {
     snprintf(name, bytes, "gemm_fp8_pair_kernel");
   } else {
-    snprintf(name, bytes, "gemm_fp8_kernel<%d>, %d a cluster, %d an SM", cut.tokens, 1 << cut.log_splits, cut.per_sm);
+    return TRDQ_ERR_CUDA;
   }
+  return TRDQ_OK;
 }
 
 trdq_status launch_gemm_fp8(const Fp8Linear& a, cudaStream_t stream) {

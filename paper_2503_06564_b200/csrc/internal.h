@@ -181,8 +181,8 @@ struct Fp8Linear {
   int32_t M, N, K, act;
 };
 trdq_status launch_gemm_fp8(const Fp8Linear& p, cudaStream_t stream);
-// what it launches there
-void describe_gemm_fp8_kernel(int32_t M, int32_t K, int32_t N, int dev, char* name, size_t bytes);
+// what it launches there; TRDQ_ERR_CUDA, as the launch itself, where none of the kernels can run
+trdq_status describe_gemm_fp8_kernel(int32_t M, int32_t K, int32_t N, int dev, char* name, size_t bytes);
 // gemm_fp8_2cta.cu: the CTA-pair kernel, and how many pairs of CTAs the device holds at once (0: it cannot run there; also when the compiler gave it other
 // registers than its split needs)
 int fp8_pair_clusters(int device);

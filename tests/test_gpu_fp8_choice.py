@@ -30,7 +30,7 @@ def test_form(form, M, N, K):
 
 def test_what_the_choice_refuses():
     from paper_2503_06564_b200 import trdq
-    for M, K, N in ((0, 256, 32), (4, 200, 32), (4, 256, 0), (4, 256, 40)):
+    for M, K, N in ((0, 256, 32), (4, 200, 32), (4, 256, 0), (4, 256, 40), (4, 131200, 32)):
         with pytest.raises(trdq.TrdqError) as e:
             trdq.trdq_kernel_choice(2, M, K, N)
         assert e.value.status == 2
